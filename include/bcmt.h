@@ -310,7 +310,8 @@ int bcmt_decode_step(const bcmt_config* cfg, const bcmt_params* params, int64_t 
 const char* bcmt_strerror(int status);
 
 /* Library version, major * 10000 + minor * 100 + patch (2.1.0: helpers
- * that create and destroy a bcmt_side's events). */
+ * that create and destroy a bcmt_side's events; 2.2.0: attention and linear
+ * attention over packed sequences). */
 int bcmt_version(void);
 
 /* ---------------------------------------------------------------- language model
@@ -384,6 +385,133 @@ int bcmt_model_train_step(const bcmt_model_config* cfg, const int32_t* tokens,
                           float* grads, float* adam_m, float* adam_v, const bcmt_adamw* opt,
                           float* loss, void* ws, size_t ws_bytes, void* stream,
                           const bcmt_side* side);
+
+/* ------------------------------------------------ attention over packed sequences
+ * Causal softmax attention of whole prompts: sequences of any lengths lie one
+ * after another in the rows of the arrays, and groups of query heads share
+ * key/value heads.  Sequence s is rows cu[s] .. cu[s+1]-1; query head h reads
+ * key/value head h / (H / Hkv); a row sees itself and the earlier rows of its
+ * own sequence:
+ *   o_t = sum_u p_tu v_u,  p_tu = exp(scale q_t.k_u - lse_t),
+ *   lse_t = log sum_u exp(scale q_t.k_u)
+ * Softmax statistics and sums are float32; in bf16 the weights p (and their
+ * gradient) are rounded to bf16 as operands of the products.
+ *
+ *   - Rows hold heads side by side: row r of q is q + r ldq, head h at h dh.  A
+ *     stride of 0 means dense rows (H dh or Hkv dh elements); otherwise it is
+ *     at least that and a multiple of 16 bytes, so q, k and v may be columns of
+ *     one projection.  o and dO share ldo; dq, dk, dv have the strides of q, k, v.
+ *   - cu: nseq + 1 int32 on the device, non-decreasing, within 0 .. total (4-byte
+ *     aligned; the host never reads it).  Sequences may be empty.  Rows before
+ *     cu[0] and from cu[nseq] on belong to no sequence and are neither read nor
+ *     written.  Values out of order or range are clamped: they give wrong rows,
+ *     never an access outside the arrays.
+ *   - A value that is not finite reaches only the rows that see it in the
+ *     forward pass; in the backward pass it may reach every gradient of its
+ *     sequence.
+ *   - Outputs must not overlap inputs or each other (columns of one array that
+ *     do not meet are fine).
+ *   - Everything is reduced in a fixed order: the same call gives the same bits.
+ *   - dh is 16, 32, 64 or 128, total <= 2^30, nseq <= 65535 (else
+ *     BCMT_ERR_UNSUPPORTED). */
+typedef struct {
+  int32_t total;               /* rows of the packed arrays, >= 1 */
+  int32_t nseq;                /* sequences, >= 1 */
+  int32_t H, Hkv;              /* query heads; key/value heads, a divisor of H */
+  int32_t dh;                  /* head width */
+  int32_t dtype;               /* bcmt_dtype of q, k, v, o and their gradients */
+  float scale;                 /* finite and > 0, usually 1 / sqrt(dh) */
+  int64_t ldq, ldk, ldv, ldo;  /* elements from a row to the next, or 0 */
+} bcmt_attn_config;
+
+/* Host-only check; BCMT_OK or a negative status. */
+int bcmt_attn_validate(const bcmt_attn_config* cfg);
+/* Bytes of scratch bcmt_attn_backward needs (the forward needs none); 0 for an
+ * invalid config. */
+size_t bcmt_attn_workspace_bytes(const bcmt_attn_config* cfg);
+/* lse: [H, total] float32, or NULL if no backward pass follows. */
+int bcmt_attn_forward(const bcmt_attn_config* cfg, const void* q, const void* k, const void* v,
+                      const int32_t* cu, void* o, float* lse, void* stream);
+/* Gradients of sum(dO * o), given the forward's o and lse.  A shared key/value
+ * head's gradient adds those of its query heads. */
+int bcmt_attn_backward(const bcmt_attn_config* cfg, const void* q, const void* k, const void* v,
+                       const int32_t* cu, const void* o, const float* lse, const void* dO,
+                       void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
+
+/* One token per sequence against a cache of keys and values.  Sequence b's cache
+ * is slot slot[b] of a pool (slot NULL: slot b), rows of position 0 .. cap-1; its
+ * length[b] earlier tokens are rows 0 .. length[b]-1.  The call writes the token's
+ * k and v to row length[b] and attends over rows 0 .. length[b]; the caller then
+ * advances the length.  Rows behind that one may hold anything.
+ * A sequence whose slot is outside the pool (a negative one marks an empty place
+ * of the batch) or whose length is negative or >= cap gets a zero output row and
+ * touches no cache.  Two sequences of a call must not share a slot.
+ * q, o: rows of H heads with strides ldq, ldo; k, v: rows of Hkv heads.  Both
+ * caches: slot s, position t, head j at s cs + t ct + j ch elements; all 0 means
+ * dense [slots, cap, Hkv, dh].  Otherwise each is positive and a multiple of 16
+ * bytes, and no two entries may overlap.  slot, length: int32 on the device. */
+typedef struct {
+  int32_t B;      /* sequences of the batch, >= 1 */
+  int32_t slots;  /* slots of the pool, >= 1 */
+  int32_t cap;    /* positions of a slot, >= 1 */
+  int32_t H, Hkv, dh, dtype;
+  float scale;
+  int64_t ldq, ldk, ldv, ldo;
+  int64_t cs, ct, ch;
+} bcmt_attn_decode_config;
+
+int bcmt_attn_decode_validate(const bcmt_attn_decode_config* cfg);
+size_t bcmt_attn_decode_workspace_bytes(const bcmt_attn_decode_config* cfg);
+int bcmt_attn_decode(const bcmt_attn_decode_config* cfg, const void* q, const void* k,
+                     const void* v, const int32_t* slot, const int32_t* length, void* kcache,
+                     void* vcache, void* o, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------ linear attention with decays
+ * A decayed sum of key-value products, one decay gamma[h] in [0, 1] per head:
+ *   S_t = gamma S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t
+ * over packed sequences (cu, strides, overlap and errors as for the attention
+ * above).  States are float32 [dh, dh] per head (rows along k, columns along v):
+ * S_in [nseq, H, dh, dh] is the state before each sequence's first row (NULL: 0),
+ * S_out the state after its last (NULL: not wanted; it may be S_in).  A prompt
+ * cut into pieces runs piece by piece on the states; an empty sequence passes its
+ * state on.  gamma: H float32 on the device (0^0 is taken as 1), 4-byte aligned;
+ * values outside [0, 1] give undefined numbers.
+ * A value that is not finite reaches only its own row and later ones. */
+typedef struct {
+  int32_t total, nseq, H, dh, dtype;
+  float scale; /* finite */
+  int64_t ldq, ldk, ldv, ldo;
+} bcmt_linattn_config;
+
+int bcmt_linattn_validate(const bcmt_linattn_config* cfg);
+/* Scratch bytes of a pass: BCMT_PASS_FORWARD or BCMT_PASS_BACKWARD. */
+size_t bcmt_linattn_workspace_bytes(const bcmt_linattn_config* cfg, int pass);
+int bcmt_linattn_forward(const bcmt_linattn_config* cfg, const void* q, const void* k,
+                         const void* v, const float* gamma, const int32_t* cu, const float* S_in,
+                         void* o, float* S_out, void* ws, size_t ws_bytes, void* stream);
+/* Gradients of sum(dO * o) + sum(dS_out * S_out).  dS_out NULL: 0; dS_in (may be
+ * dS_out) and dgamma [H] (float32, summed over all rows and sequences) NULL: not
+ * wanted. */
+int bcmt_linattn_backward(const bcmt_linattn_config* cfg, const void* q, const void* k,
+                          const void* v, const float* gamma, const int32_t* cu,
+                          const float* S_in, const void* dO, const float* dS_out, void* dq,
+                          void* dk, void* dv, float* dS_in, float* dgamma, void* ws,
+                          size_t ws_bytes, void* stream);
+
+/* One token per sequence: the state of slot slot[b] (NULL: b) of a pool S_in
+ * [slots, H, dh, dh] advances into the same slot of S_out (which may be S_in; other
+ * slots of S_out are not written).  A slot outside the pool gives a zero output row
+ * and touches no state; two sequences must not share a slot. */
+typedef struct {
+  int32_t B, slots, H, dh, dtype;
+  float scale;
+  int64_t ldq, ldk, ldv, ldo;
+} bcmt_linattn_step_config;
+
+int bcmt_linattn_step_validate(const bcmt_linattn_step_config* cfg);
+int bcmt_linattn_step(const bcmt_linattn_step_config* cfg, const void* q, const void* k,
+                      const void* v, const float* gamma, const int32_t* slot, const float* S_in,
+                      float* S_out, void* o, void* stream);
 
 /* ---- Stage tracing (profiling aid) -------------------------------------
  * While tracing is on, every kernel launch of bcmt_layer_forward and

@@ -404,7 +404,7 @@ const char* bcmt_strerror(int status) {
   }
 }
 
-int bcmt_version(void) { return 20100; }
+int bcmt_version(void) { return 20200; }
 
 int bcmt_side_events_create(bcmt_side* side) {
   if (!side) return BCMT_ERR_INVALID;

@@ -250,6 +250,13 @@ __device__ __forceinline__ bf16x8 lds_read_b128(const bf16* p) {
   asm volatile("ds_read_b128 %0, %1" : "=v"(v) : "v"(a));
   return v;
 }
+// 8-byte bf16 LDS read in inline assembly; same contract as lds_read_tr().
+__device__ __forceinline__ bf16x4 lds_read_b64(const bf16* p) {
+  bf16x4 v;
+  const unsigned a = (unsigned)(uintptr_t)((__attribute__((address_space(3))) bf16*)(p));
+  asm volatile("ds_read_b64 %0, %1" : "=v"(v) : "v"(a));
+  return v;
+}
 // The same reads at a byte address plus an immediate offset.
 template <int OFF>
 __device__ __forceinline__ bf16x4 lds_read_tr_at(unsigned a) {

@@ -379,4 +379,81 @@ hipError_t dec_pool(DType dt, const void* Hc, const float* spc, float* N, const 
 hipError_t dec_mem_finish(const float* part, int ks, float* C, float* Z, int B, int D, float gamma,
                           const float* gvec, hipStream_t s);
 
+// ------------------------------------------------------------------ sequence mixers
+// Packed sequences: rows [cu[s], cu[s+1]) of arrays of `total` rows; strides in
+// elements between rows, heads side by side within a row.
+struct SeqAttn {
+  const void *q, *k, *v;
+  const int* cu;
+  void* o;     // forward: written; backward: read
+  float* lse;  // [H, total] natural logarithm; forward: may be null
+  const void* dout;
+  void *dq, *dk, *dv;  // strides of q, k, v
+  float* delta;        // scratch [H, total]
+  int total, nseq, H, Hkv;
+  int64_t ldq, ldk, ldv, ldo;  // ldo: o and dout
+  float scale;
+};
+hipError_t seq_attn_fwd(DType dt, int dh, const SeqAttn& a, hipStream_t s);
+hipError_t seq_attn_bwd(DType dt, int dh, const SeqAttn& a, hipStream_t s);
+
+// One token per sequence against caches [slots][cap] of Hkv heads.
+struct DecAttn {
+  const void *q, *k, *v;
+  const int *slot, *length;  // slot may be null (sequence b in slot b)
+  void *kcache, *vcache, *o;
+  float *part_o, *part_ml;  // [B, H, nsplit, dh] and [B, H, nsplit, 2]
+  int B, slots, cap, H, Hkv, nsplit;
+  int64_t ldq, ldk, ldv, ldo, cs, ct, ch;  // cache strides: slot, token, head
+  float sl2;                               // scale / ln 2
+};
+int seq_attn_decode_splits(DType dt, int dh, int B, int H, int Hkv, int cap);
+hipError_t seq_attn_decode(DType dt, int dh, const DecAttn& a, hipStream_t s);
+
+// Linear attention with one decay per head: one pass of the operator over rows
+// a (queries), b (keys), c (values), with strides in elements.
+struct LinPass {
+  const void *a, *b, *c;
+  void* out;
+  const int* cu;
+  const float* gamma;   // [H]
+  const float* s_in;    // [nseq, H, dh, dh] or null (0)
+  float* s_out;         // the same, or null
+  float* seg_state;     // scratch [total / seg + 1, H, dh, dh]: states between segments
+  float* given;         // the same size: copies of s_in, or null (s_out is not s_in)
+  int sr, sc;           // strides of s_in, s_out and (as read) seg_state: b's width, c's width
+  int total, nseq, H, seg;  // seg: rows of a segment, a multiple of 64
+  int64_t lda, ldb, ldc, ldo;
+  float s_intra, s_inter, s_upd;  // factors of the scores, of the state's term, of its update
+};
+// state: only the segments' own sums -> seg_state (rows b, columns c).
+hipError_t lin_pass(DType dt, int dh, const LinPass& a, bool rev, bool state, hipStream_t s);
+// Those sums -> the states at the boundaries between segments (s_in unswapped).
+hipError_t lin_scan(int dh, const LinPass& a, bool rev, hipStream_t s);
+int lin_segment_rows(int total, int H);
+
+struct LinDecay {
+  const void *q, *k, *v, *dout;
+  const int* cu;
+  const float *gamma, *s_in, *ds_out, *seg_s, *seg_r;  // states of sequences, of boundaries
+  float* part;    // scratch [H, nslot, dh / 16]
+  float* dgamma;  // [H]
+  int total, nseq, H, seg, nslot;
+  int64_t ldq, ldk, ldv, ldo;
+  float scale;
+};
+hipError_t lin_dgamma(DType dt, int dh, const LinDecay& a, hipStream_t s);
+
+struct LinStep {
+  const void *q, *k, *v;
+  const float *gamma, *s_in;
+  const int* slot;  // or null (sequence b in slot b)
+  float* s_out;     // may be s_in
+  void* o;
+  int B, slots, H;
+  int64_t ldq, ldk, ldv, ldo;
+  float scale;
+};
+hipError_t lin_step(DType dt, int dh, const LinStep& a, hipStream_t s);
+
 }  // namespace bcmt

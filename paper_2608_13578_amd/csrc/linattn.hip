@@ -1,0 +1,647 @@
+// Linear attention with one decay per head over packed sequences.
+//
+//   S_t = g S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t
+// Chunked form, for a chunk of C rows with local index i = 0 .. C-1 and the
+// state S before it:
+//   o_i = scale (sum_{j <= i} g^(i-j) (q_i . k_j) v_j  +  g^(i+1) S^T q_i)
+//   S' = g^C S + sum_j g^(C-1-j) k_j v_j^T
+// The gradients are the same operator.  With R the gradient of the state
+// after a chunk (R' the one of the state before it):
+//   dq_i = scale (sum_{j <= i} g^(i-j) (do_i . v_j) k_j + g^(i+1) S do_i)
+//   dk_j = scale sum_{i >= j} g^(i-j) (v_j . do_i) q_i + g^(C-1-j) R v_j
+//   dv_j = scale sum_{i >= j} g^(i-j) (k_j . q_i) do_i + g^(C-1-j) R^T k_j
+//   R' = g^C R + scale sum_i g^(i+1) q_i do_i^T
+// so one kernel takes rows a (queries), b (keys), c (values) of any of the
+// three and a direction: in reverse, the local index i' = C-1-i makes the state
+// terms g^i' and g^(C-i') instead of g^(i+1) and g^(C-1-j).
+//
+// A workgroup owns one head of one segment of a sequence and walks its chunks
+// of 64 rows in order.  Wave w owns columns 16w .. 16w+15 of the value width
+// and keeps its part of the state, [DH][16] in float32, in registers in the
+// layout of a product's result, which is also the layout of a product's first
+// operand: the state never leaves the registers between chunks.  The masked,
+// decayed scores of a chunk are shared through LDS.
+//
+// The sum of a state takes its weighted rows g^n c_j in three bf16 parts
+// (24 bits), so that a float32 state loses nothing to bf16 products; scores and
+// the state as an operand of a bf16 output are rounded to bf16 once, an error
+// below the output's own rounding.
+//
+// Long sequences are cut into segments of `seg` rows that run side by side:
+// their own sums first (lin_kernel<..., STATE>), then a scan over a sequence's
+// segments, which leaves the state at every boundary between two segments.
+// Boundary k >= 1 of a sequence that begins at row b is entry b / seg + k of the
+// array: distinct for all boundaries, at most total / seg, and sequences of one
+// segment have none.
+#include "kernels.h"
+#include "mixer_tile.h"
+
+namespace bcmt {
+namespace {
+
+constexpr int kC = 64;  // rows of a chunk
+
+__device__ __forceinline__ float powg(float lg2, int e) {  // g^e; 0^0 = 1
+  return e == 0 ? 1.f : exp2_fast(lg2 * (float)e);
+}
+
+template <typename T> struct Parts;  // exact enough operands of a float32 sum
+template <> struct Parts<float> { static constexpr int N = 1; };
+template <> struct Parts<bf16> { static constexpr int N = 3; };
+
+__device__ __forceinline__ void split(const float (&x)[8], f32x8 (&p)[1]) {
+  p[0] = f32x8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&p)[3]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const bf16 a = (bf16)x[e];
+    const float r = x[e] - (float)a;
+    const bf16 b = (bf16)r;
+    p[0][e] = a;
+    p[1][e] = b;
+    p[2][e] = (bf16)(r - (float)b);
+  }
+}
+
+// Elements 4g .. + 3 and 16 + 4g .. + 3 of the 32 from c0 of a row (one half if
+// the row has 16): the order in which two state tiles hold them.
+template <typename T> struct HalfRaw;
+template <> struct HalfRaw<bf16> { bf16x4 a, b; };
+template <> struct HalfRaw<float> { f32x4 a, b; };
+template <typename T, int DH>
+__device__ __forceinline__ HalfRaw<T> row8p(const T* t, int r, int c0, int lane) {
+  const int g = lane >> 4, c1 = DH >= 32 ? c0 + 16 : c0;
+  const T *p = t + Tile<T, DH>::off(r, c0 + 4 * g), *q = t + Tile<T, DH>::off(r, c1 + 4 * g);
+  if constexpr (sizeof(T) == 2) return {lds_read_b64(p), lds_read_b64(q)};
+  else return {lds_read_f32x4(p), lds_read_f32x4(q)};
+}
+template <typename T, int DH>
+__device__ __forceinline__ typename Frag<T>::type take_row8p(HalfRaw<T>& r) {
+  lds_tr_bind(r.a);
+  lds_tr_bind(r.b);
+  const auto b = DH >= 32 ? r.b : decltype(r.b){};
+  return {r.a[0], r.a[1], r.a[2], r.a[3], b[0], b[1], b[2], b[3]};
+}
+
+// state += (rows a)^T (weighted rows c): this wave's 16 columns, the 64 rows
+// of a chunk.  w: weights of the 8 rows lane / 16 holds in each half chunk; a
+// zero weight drops its row whatever it holds.
+template <typename T, int DH>
+__device__ __forceinline__ void add_outer(f32x4 (&S)[DH / 16], const T* At,
+                                          const typename Frag<T>::type (&cf)[2],
+                                          const float (&w)[2][8], int lane) {
+  typedef typename Frag<T>::type F;
+  constexpr int NP = Parts<T>::N;
+#pragma unroll
+  for (int us = 0; us < 2; ++us) {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = w[us][e] == 0.f ? 0.f : w[us][e] * to_f32(cf[us][e]);
+    F p[NP];
+    split(x, p);
+#pragma unroll
+    for (int t = 0; t < DH / 16; ++t) {
+      ColRaw<T> ar = Tile<T, DH>::col8(At, us * 32, us * 32 + 16, t * 16, lane);
+      lds_tr_wait();
+      const F a = take(ar);
+#pragma unroll
+      for (int n = NP - 1; n >= 0; --n) S[t] = mma16(a, p[n], S[t]);
+    }
+  }
+}
+
+// The wave's part of a [DH][DH] state in memory: rows 16t + 4g + r, column col.
+template <int NT>
+__device__ __forceinline__ void load_state(f32x4 (&S)[NT], const float* p, int sr, int sc, int col,
+                                           int lg) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) S[t][r] = p[(16 * t + 4 * lg + r) * sr + col * sc];
+}
+template <int NT>
+__device__ __forceinline__ void store_state(const f32x4 (&S)[NT], float* p, int sr, int sc, int col,
+                                            int lg) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[(16 * t + 4 * lg + r) * sr + col * sc] = S[t][r];
+}
+
+struct LinSeg {
+  int seq, n, t0, len, row0;  // sequence; its length; segment [t0, t0 + len); first row
+  int bound;                  // entry of the boundary before it; the one after it follows
+  int first;                  // entry of the sequence's first boundary
+  bool last;                  // the sequence's last segment
+};
+// Segment of slot x (segments are tiles of `seg` rows from the sequence's
+// start); len < 0: an empty slot.  An empty sequence has one segment of no rows.
+__device__ __forceinline__ LinSeg lin_segment(const int* cu, int nseq, int total, int seg, int slot) {
+  const SeqTile st = find_tile(cu, nseq, total, seg, slot);
+  LinSeg r;
+  r.seq = st.seq;
+  r.n = st.end - st.begin;
+  r.t0 = st.tile * seg;
+  r.len = min(seg, r.n - r.t0);
+  if (st.tile < 0 || (st.tile > 0 && r.len <= 0)) r.len = -1;
+  r.row0 = st.begin + r.t0;
+  r.bound = st.begin / seg + st.tile;
+  r.first = st.begin / seg + 1;
+  r.last = r.t0 + seg >= r.n;
+  return r;
+}
+
+// ------------------------------------------------------------------ the operator
+// REV: rows in reverse.  STATE: only the segment's own sum of states.
+
+template <typename T, int DH, bool REV, bool STATE>
+__global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
+  typedef typename Frag<T>::type F;
+  typedef Tile<T, DH> TL;
+  typedef Tile<T, kC> TP;
+  constexpr int NW = DH / 16, NT = DH / 16, KS = DH >= 32 ? DH / 32 : 1;
+  constexpr int NB = sizeof(T) * DH > 256 ? 1 : 2;  // buffers: LDS of three tiles each
+  constexpr int FIRST = STATE ? 1 : 0;              // tiles a, b, c: the sum needs b and c
+  constexpr int NI = TL::NCH / NW;  // loads of a tile by each wave
+  __shared__ __attribute__((aligned(1024))) T lds[NB][3 - FIRST][kC * DH];
+  __shared__ __attribute__((aligned(1024))) T P[STATE ? 16 : kC * kC];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lr = lane & 15, lg = lane >> 4;
+  const int h = blockIdx.x % a.H;
+  const LinSeg sg = lin_segment(a.cu, a.nseq, a.total, a.seg, blockIdx.x / a.H);
+  if (sg.len < 0) return;
+  // the sum of a segment that no other follows is not needed
+  if (STATE && (REV ? sg.t0 == 0 : sg.last)) return;
+  const float lg2 = log2f(a.gamma[h]);
+  const int col = wave * 16 + lr;
+
+  f32x4 S[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) S[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int64_t sq = ((int64_t)sg.seq * a.H + h) * DH * DH;
+  const int64_t dd = (int64_t)a.H * DH * DH;
+  float* bs = a.seg_state + sg.bound * dd + (int64_t)h * DH * DH;  // the boundary before; + dd: after
+  if (!STATE) {
+    if (REV ? !sg.last : sg.t0 > 0) load_state<NT>(S, REV ? bs + dd : bs, a.sr, a.sc, col, lg);
+    else if (a.given && !(REV ? sg.t0 == 0 : sg.last))
+      load_state<NT>(S, a.given + sg.first * dd + (int64_t)h * DH * DH, a.sr, a.sc, col, lg);
+    else if (a.s_in) load_state<NT>(S, a.s_in + sq, a.sr, a.sc, col, lg);
+  }
+  const int nc = (sg.len + kC - 1) / kC;
+  const int64_t r0 = REV ? sg.row0 + sg.len - 1 : sg.row0;
+  const int64_t la = REV ? -a.lda : a.lda, lb = REV ? -a.ldb : a.ldb, lc = REV ? -a.ldc : a.ldc;
+  const T* A = STATE ? nullptr : (const T*)a.a + r0 * a.lda + h * DH;
+  const T* B = (const T*)a.b + r0 * a.ldb + h * DH;
+  const T* Cc = (const T*)a.c + r0 * a.ldc + h * DH;
+  auto issue = [=](int c) __attribute__((always_inline)) {
+    const int buf = NB == 2 ? c & 1 : 0;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int ti = wave * NI + i;
+      if (!STATE) TL::issue(A, la, c * kC, sg.len - 1, lds[buf][0], ti, lane);
+      TL::issue(B, lb, c * kC, sg.len - 1, lds[buf][1 - FIRST], ti, lane);
+      TL::issue(Cc, lc, c * kC, sg.len - 1, lds[buf][2 - FIRST], ti, lane);
+    }
+  };
+  // g^(64 - 1 - j) (forward) or g^(64 - j) (reverse) for the rows this lane
+  // holds in each half chunk; the row factors of the state's term
+  constexpr int EI = REV ? 0 : 1, EU = REV ? 1 : 0;
+  float w[2][8], fi[4];
+  auto weights = [&](int len) __attribute__((always_inline)) {
+#pragma unroll
+    for (int us = 0; us < 2; ++us)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int j = us * 32 + (e < 4 ? 4 * lg + e : 12 + 4 * lg + e);
+        w[us][e] = j < len ? a.s_upd * powg(lg2, len - 1 - j + EU) : 0.f;
+      }
+  };
+  weights(kC);
+#pragma unroll
+  for (int ib = 0; ib < 4; ++ib) fi[ib] = a.s_inter * powg(lg2, ib * 16 + lr + EI);
+  const float gC = powg(lg2, kC);
+
+  if (NB == 2 && nc > 0) {
+    issue(0);
+    vm_wait<0>();
+  }
+  for (int c = 0; c < nc; ++c) {
+    wg_barrier();  // this chunk's tiles are there; every wave is done with the last chunk
+    if (NB == 2) {
+      if (c + 1 < nc) issue(c + 1);
+    } else {
+      issue(c);
+      vm_wait<0>();
+      wg_barrier();
+    }
+    const T* At = lds[NB == 2 ? c & 1 : 0][0];
+    const T* Bt = lds[NB == 2 ? c & 1 : 0][1 - FIRST];
+    const T* Ct = lds[NB == 2 ? c & 1 : 0][2 - FIRST];
+    const int len = min(kC, sg.len - c * kC);
+    f32x4 oa[4];
+    F cf[2];
+    if constexpr (!STATE) {
+      // scores of 16 x 16 blocks (ib, jb), jb <= ib, and the zero blocks beside
+      // the diagonal; row i of P holds the keys of a half chunk in the order of
+      // Tile::col8
+#pragma unroll 1
+      for (int blk = wave; blk < 12; blk += NW) {
+        // blocks 0..9: the triangle by rows; 10, 11: (0, 1) and (2, 3)
+        const int ib = blk < 10 ? (blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0) : (blk - 10) * 2;
+        const int jb = blk < 10 ? blk - ib * (ib + 1) / 2 : ib + 1;
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        if (blk < 10) {
+          RowRaw<T> br[KS], ar[KS];
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) {
+            br[ds] = TL::row8(Bt, jb * 16 + lr, ds * 32 + lg * 8);
+            ar[ds] = TL::row8(At, ib * 16 + lr, ds * 32 + lg * 8);
+          }
+          lds_tr_wait();
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) {
+            const F bf = TL::take_row(br[ds], ds * 32 + lg * 8);
+            s = mma16(bf, TL::take_row(ar[ds], ds * 32 + lg * 8), s);
+          }
+        }
+        const int i = ib * 16 + lr;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int j = jb * 16 + lg * 4 + r;
+          s[r] = blk < 10 && j <= i && j < len ? s[r] * a.s_intra * powg(lg2, i - j) : 0.f;
+        }
+        store4(P + TP::off(i, (jb >> 1) * 32 + 8 * lg + 4 * (jb & 1)), s[0], s[1], s[2], s[3]);
+      }
+      // the state's term, while the scores arrive
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib) oa[ib] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const F sf = frag_from<T>(S[2 * ks], DH >= 32 ? S[2 * ks + (DH >= 32)] : f32x4{});
+        HalfRaw<T> qr[4];
+#pragma unroll
+        for (int ib = 0; ib < 4; ++ib) qr[ib] = row8p<T, DH>(At, ib * 16 + lr, ks * 32, lane);
+        lds_tr_wait();
+#pragma unroll
+        for (int ib = 0; ib < 4; ++ib) oa[ib] = mma16(sf, take_row8p<T, DH>(qr[ib]), oa[ib]);
+      }
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib) oa[ib] *= fi[ib];
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the scores are written
+      wg_barrier();
+    }
+    ColRaw<T> cr[2];
+#pragma unroll
+    for (int us = 0; us < 2; ++us) cr[us] = TL::col8(Ct, us * 32, us * 32 + 16, wave * 16, lane);
+    lds_tr_wait();
+#pragma unroll
+    for (int us = 0; us < 2; ++us) cf[us] = take(cr[us]);
+    if constexpr (!STATE) {
+      // A value that is not finite must not reach the rows before it through
+      // 0 * inf: such columns are summed row by row.
+      if (__ballot((nonfinite_bits(cf[0]) | nonfinite_bits(cf[1])) != 0) == 0) {
+#pragma unroll
+        for (int ib = 0; ib < 4; ++ib) {
+          RowRaw<T> pr[2];
+#pragma unroll
+          for (int us = 0; us <= ib / 2; ++us) pr[us] = TP::row8(P, ib * 16 + lr, us * 32 + lg * 8);
+          lds_tr_wait();
+#pragma unroll
+          for (int us = 0; us <= ib / 2; ++us) oa[ib] = mma16(cf[us], take(pr[us]), oa[ib]);
+        }
+      } else {
+#pragma unroll
+        for (int ib = 0; ib < 4; ++ib) {
+          const int i = ib * 16 + lr;
+#pragma unroll 1
+          for (int j = 0; j <= min(i, len - 1); ++j) {
+            const int pos = (j & 32) + 8 * ((j >> 2) & 3) + ((j >> 4) & 1) * 4 + (j & 3);
+            const float p = to_f32(P[TP::off(i, pos)]);
+            const f32x4 vv = load4f(Ct + TL::off(j, wave * 16 + lg * 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) oa[ib][e] = fmaf(p, vv[e], oa[ib][e]);
+          }
+        }
+      }
+    }
+    // the state after the chunk, unless nothing reads it
+    if (STATE || c + 1 < nc || a.s_out) {
+      float g = gC;
+      if (len < kC) {
+        weights(len);
+        g = powg(lg2, len);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) S[t] *= g;
+      add_outer<T, DH>(S, Bt, cf, w, lane);
+    }
+    if (NB == 2) vm_wait<0>();  // the next chunk's tiles, before the stores
+    if constexpr (!STATE) {
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib) {
+        const int i = ib * 16 + lr;
+        if (i < len)
+          store4((T*)a.out + (r0 + (REV ? -1 : 1) * (int64_t)(c * kC + i)) * a.ldo + h * DH +
+                     wave * 16 + lg * 4,
+                 oa[ib][0], oa[ib][1], oa[ib][2], oa[ib][3]);
+      }
+    }
+  }
+  if (STATE) store_state<NT>(S, REV ? bs : bs + dd, DH, 1, col, lg);
+  else if (a.s_out && (REV ? sg.t0 == 0 : sg.last))
+    store_state<NT>(S, a.s_out + sq, a.sr, a.sc, col, lg);
+}
+
+// The segments' own sums -> the states at the boundaries, in place, from the
+// sequence's given state.  `given`, if the operator writes its last state over the
+// given one (by another workgroup than the one that reads it), keeps a copy at the
+// sequence's first boundary.  Forward: the sum of segment i lies at the boundary
+// after it; reverse: at the one before it.  One thread per four elements.
+template <bool REV>
+__global__ __launch_bounds__(256) void lin_scan_kernel(const int* __restrict__ cu, int nseq,
+                                                       int total, int seg, int H, int dd,
+                                                       const float* __restrict__ gamma,
+                                                       const float* __restrict__ s_in,
+                                                       float* __restrict__ seg_state,
+                                                       float* __restrict__ given) {
+  const int h = blockIdx.y;
+  const int e = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (e >= dd) return;
+  const float lg2 = log2f(gamma[h]);
+  for (int seq = blockIdx.z; seq < nseq; seq += gridDim.z) {
+    const int begin = min(max(cu[seq], 0), total), end = min(max(cu[seq + 1], begin), total);
+    const int n = end - begin, ns = (n + seg - 1) / seg;
+    if (ns < 2) continue;
+    f32x4 u = {0.f, 0.f, 0.f, 0.f};
+    if (s_in) u = *(const f32x4*)(s_in + ((int64_t)seq * H + h) * dd + e);
+    if (given) *(f32x4*)(given + ((int64_t)(begin / seg + 1) * H + h) * dd + e) = u;
+    for (int i = 1; i < ns; ++i) {
+      const int k = REV ? ns - i : i;  // boundary; the segment just passed
+      const int len = REV ? min(seg, n - k * seg) : seg;
+      float* p = seg_state + ((int64_t)(begin / seg + k) * H + h) * dd + e;
+      u = u * powg(lg2, len) + *(const f32x4*)p;
+      *(f32x4*)p = u;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ decay gradient
+// dg = sum_t <R_t, S_{t-1}>, per segment from the state S before it and the
+// gradient R of the state after it: with D = dS / dg from 0 at the segment's
+// start,
+//   dg_seg = sum_t scale do_t . (D_t^T q_t) + <R, D_end>
+// chunk by chunk:
+//   sum_{j < i} (i-j) g^(i-j-1) scale (q_i . k_j) (do_i . v_j)
+//   + <S, scale sum_i (i+1) g^i q_i do_i^T> + <D, scale sum_i g^(i+1) q_i do_i^T>
+//   D' = g^C D + C g^(C-1) S + sum_j (C-1-j) g^(C-2-j) k_j v_j^T
+// Both inner products take the states from float32 registers and the sums in
+// parts.  One partial sum per wave, added in a fixed order at the end.
+
+template <typename T, int DH>
+__global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
+  typedef typename Frag<T>::type F;
+  typedef Tile<T, DH> TL;
+  constexpr int NW = DH / 16, NT = DH / 16, KS = DH >= 32 ? DH / 32 : 1;
+  constexpr int NI = TL::NCH / NW;
+  __shared__ __attribute__((aligned(1024))) T lds[4][kC * DH];  // q, k, v, do
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lr = lane & 15, lg = lane >> 4;
+  const int h = blockIdx.x % a.H, slot = blockIdx.x / a.H;
+  const LinSeg sg = lin_segment(a.cu, a.nseq, a.total, a.seg, slot);
+  float* out = a.part + ((int64_t)h * a.nslot + slot) * NW + wave;
+  if (sg.len <= 0) {
+    // an empty slot, or an empty sequence: the state passes through unchanged
+    if (lane == 0) *out = 0.f;
+    return;
+  }
+  const float lg2h = log2f(a.gamma[h]);
+  const int col = wave * 16 + lr;
+  f32x4 S[NT], D[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    S[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    D[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int64_t sq = ((int64_t)sg.seq * a.H + h) * DH * DH;
+  const int64_t dd = (int64_t)a.H * DH * DH, bd = sg.bound * dd + (int64_t)h * DH * DH;
+  if (sg.t0 > 0) load_state<NT>(S, a.seg_s + bd, DH, 1, col, lg);
+  else if (a.s_in) load_state<NT>(S, a.s_in + sq, DH, 1, col, lg);
+
+  const T* qs = (const T*)a.q + sg.row0 * a.ldq + h * DH;
+  const T* ks_ = (const T*)a.k + sg.row0 * a.ldk + h * DH;
+  const T* vs = (const T*)a.v + sg.row0 * a.ldv + h * DH;
+  const T* ds_ = (const T*)a.dout + sg.row0 * a.ldo + h * DH;
+  float sum = 0.f;
+  const int nc = (sg.len + kC - 1) / kC;
+  for (int c = 0; c < nc; ++c) {
+    wg_barrier();
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int ti = wave * NI + i;
+      TL::issue(qs, a.ldq, c * kC, sg.len - 1, lds[0], ti, lane);
+      TL::issue(ks_, a.ldk, c * kC, sg.len - 1, lds[1], ti, lane);
+      TL::issue(vs, a.ldv, c * kC, sg.len - 1, lds[2], ti, lane);
+      TL::issue(ds_, a.ldo, c * kC, sg.len - 1, lds[3], ti, lane);
+    }
+    vm_wait<0>();
+    wg_barrier();
+    const int len = min(kC, sg.len - c * kC);
+    float lg2 = lg2h;  // opaque, so that no table of powers is kept in registers
+    asm volatile("" : "+v"(lg2));
+#pragma unroll 1
+    for (int blk = wave; blk < 10; blk += NW) {
+      const int ib = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, jb = blk - ib * (ib + 1) / 2;
+      f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ds = 0; ds < KS; ++ds) {
+        const int c0 = ds * 32 + lg * 8;
+        RowRaw<T> qr = TL::row8(lds[0], ib * 16 + lr, c0), kr = TL::row8(lds[1], jb * 16 + lr, c0);
+        RowRaw<T> vr = TL::row8(lds[2], jb * 16 + lr, c0), dr = TL::row8(lds[3], ib * 16 + lr, c0);
+        lds_tr_wait();
+        const F kf = TL::take_row(kr, c0), vf = TL::take_row(vr, c0);
+        s = mma16(kf, TL::take_row(qr, c0), s);
+        dp = mma16(vf, TL::take_row(dr, c0), dp);
+      }
+      const int i = ib * 16 + lr;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = jb * 16 + lg * 4 + r;
+        if (j < i && i < len) sum += a.scale * s[r] * dp[r] * (float)(i - j) * powg(lg2, i - j - 1);
+      }
+    }
+    ColRaw<T> dr[2], vr[2];
+    F df[2], vf[2];
+#pragma unroll
+    for (int us = 0; us < 2; ++us) {
+      dr[us] = TL::col8(lds[3], us * 32, us * 32 + 16, wave * 16, lane);
+      vr[us] = TL::col8(lds[2], us * 32, us * 32 + 16, wave * 16, lane);
+    }
+    lds_tr_wait();
+#pragma unroll
+    for (int us = 0; us < 2; ++us) {
+      df[us] = take(dr[us]);
+      vf[us] = take(vr[us]);
+    }
+    // weights of the rows this lane holds: row(us, e)
+    float w[2][8];
+    auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int us = 0; us < 2; ++us)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = us * 32 + (e < 4 ? 4 * lg + e : 12 + 4 * lg + e);
+          w[us][e] = j < len ? f(j) : 0.f;
+        }
+    };
+    f32x4 W[NT];
+    auto inner = [&](const f32x4(&x)[NT]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += W[t][r] * x[t][r];
+    };
+#pragma unroll
+    for (int t = 0; t < NT; ++t) W[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    each([&](int i) { return a.scale * (float)(i + 1) * powg(lg2, i); });
+    add_outer<T, DH>(W, lds[0], df, w, lane);
+    inner(S);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) W[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    each([&](int i) { return a.scale * powg(lg2, i + 1); });
+    add_outer<T, DH>(W, lds[0], df, w, lane);
+    inner(D);
+    const float g = powg(lg2, len), g1 = (float)len * powg(lg2, len - 1);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      D[t] = D[t] * g + S[t] * g1;
+      S[t] *= g;
+    }
+    each([&](int j) { return j < len - 1 ? (float)(len - 1 - j) * powg(lg2, len - 2 - j) : 0.f; });
+    add_outer<T, DH>(D, lds[1], vf, w, lane);
+    each([&](int j) { return powg(lg2, len - 1 - j); });
+    add_outer<T, DH>(S, lds[1], vf, w, lane);
+  }
+  const float* R = !sg.last ? a.seg_r + bd + dd : a.ds_out ? a.ds_out + sq : nullptr;
+  if (R) {
+    load_state<NT>(S, R, DH, 1, col, lg);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum += S[t][r] * D[t][r];
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) *out = sum;
+}
+
+// dgamma[h] = sum of its partials, in a fixed order.
+__global__ __launch_bounds__(256) void lin_dgamma_sum_kernel(const float* __restrict__ part, int n,
+                                                             float* __restrict__ dgamma) {
+  __shared__ float red[4];
+  const float* p = part + (int64_t)blockIdx.x * n;
+  float s = 0.f;
+  for (int i = threadIdx.x; i < n; i += 256) s += p[i];
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) dgamma[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// ------------------------------------------------------------------ single tokens
+// S' = g S + k v^T, o = scale S'^T q: each state is read and written once, in
+// 16-byte vectors along its columns; the rows of a head are spread over the
+// workgroup and their products with q joined in LDS.
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void lin_step_kernel(LinStep a) {
+  constexpr int CV = DH / 4, NR = 256 / CV;  // vectors of a row; rows at a time
+  __shared__ __attribute__((aligned(16))) float red[NR][DH];
+  const int h = blockIdx.x % a.H, b = blockIdx.x / a.H;
+  const int c = (threadIdx.x % CV) * 4, r0 = threadIdx.x / CV;
+  const int slot = a.slot ? a.slot[b] : b;
+  T* o = (T*)a.o + (int64_t)b * a.ldo + h * DH;
+  if (slot < 0 || slot >= a.slots) {
+    if (r0 == 0) store4(o + c, 0.f, 0.f, 0.f, 0.f);
+    return;
+  }
+  const T* q = (const T*)a.q + (int64_t)b * a.ldq + h * DH;
+  const T* k = (const T*)a.k + (int64_t)b * a.ldk + h * DH;
+  const f32x4 v = load4f((const T*)a.v + (int64_t)b * a.ldv + h * DH + c);
+  const int64_t base = ((int64_t)slot * a.H + h) * DH * DH + c;
+  const float g = a.gamma[h];
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < (DH + NR - 1) / NR; ++i) {
+    const int r = i * NR + r0;
+    if (NR <= DH || r < DH) {
+      f32x4 s = *(const f32x4*)(a.s_in + base + r * DH);
+      const float kr = to_f32(k[r]), qr = to_f32(q[r]);
+      s = s * g + v * kr;
+      *(f32x4*)(a.s_out + base + r * DH) = s;
+      acc += s * qr;
+    }
+  }
+  *(f32x4*)&red[r0][c] = acc;
+  __syncthreads();
+  for (int x = threadIdx.x; x < DH; x += 256) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) s += red[i][x];
+    o[x] = from_f32<T>(s * a.scale);
+  }
+}
+
+template <typename T, int DH>
+hipError_t pass_t(const LinPass& a, bool rev, bool state, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)(a.total / a.seg + a.nseq) * a.H));
+  if (rev && state) lin_kernel<T, DH, true, true><<<grid, DH * 4, 0, s>>>(a);
+  else if (rev) lin_kernel<T, DH, true, false><<<grid, DH * 4, 0, s>>>(a);
+  else if (state) lin_kernel<T, DH, false, true><<<grid, DH * 4, 0, s>>>(a);
+  else lin_kernel<T, DH, false, false><<<grid, DH * 4, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <typename T, int DH>
+hipError_t dgamma_t(const LinDecay& a, hipStream_t s) {
+  lin_dgamma_kernel<T, DH><<<dim3((unsigned)((int64_t)a.nslot * a.H)), DH * 4, 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  lin_dgamma_sum_kernel<<<dim3(a.H), 256, 0, s>>>(a.part, a.nslot * (DH / 16), a.dgamma);
+  return hipGetLastError();
+}
+template <typename T, int DH>
+hipError_t step_t(const LinStep& a, hipStream_t s) {
+  lin_step_kernel<T, DH><<<dim3((unsigned)((int64_t)a.B * a.H)), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t lin_pass(DType dt, int dh, const LinPass& a, bool rev, bool state, hipStream_t s) {
+  BY_TYPE_AND_WIDTH(pass_t, dt, dh, a, rev, state, s);
+}
+hipError_t lin_scan(int dh, const LinPass& a, bool rev, hipStream_t s) {
+  const dim3 grid((dh * dh / 4 + 255) / 256, a.H, a.nseq < 64 ? a.nseq : 64);
+  if (rev)
+    lin_scan_kernel<true><<<grid, 256, 0, s>>>(a.cu, a.nseq, a.total, a.seg, a.H, dh * dh, a.gamma,
+                                               a.s_in, a.seg_state, a.given);
+  else
+    lin_scan_kernel<false><<<grid, 256, 0, s>>>(a.cu, a.nseq, a.total, a.seg, a.H, dh * dh, a.gamma,
+                                                a.s_in, a.seg_state, a.given);
+  return hipGetLastError();
+}
+hipError_t lin_dgamma(DType dt, int dh, const LinDecay& a, hipStream_t s) {
+  BY_TYPE_AND_WIDTH(dgamma_t, dt, dh, a, s);
+}
+hipError_t lin_step(DType dt, int dh, const LinStep& a, hipStream_t s) {
+  BY_TYPE_AND_WIDTH(step_t, dt, dh, a, s);
+}
+
+// Rows of a segment: about 512 workgroups over all heads, at least 256 rows (a
+// boundary's state, written twice and read twice, costs the traffic of a few
+// chunks).
+int lin_segment_rows(int total, int H) {
+  const int64_t want = ((int64_t)total * H / 512 + kC - 1) / kC * kC;
+  return (int)(want < 256 ? 256 : want);
+}
+
+}  // namespace bcmt

@@ -1,0 +1,188 @@
+// LDS tiles and packed-sequence lookup shared by the sequence mixers
+// (packed attention and linear attention).
+//
+// A tile is ROWS rows of one head, [ROWS][DH] in its natural layout, filled by
+// direct global->LDS loads of 16-byte chunks.  Chunk c of row r lies at chunk
+// c ^ swz(r) of its row.  The 64 LDS banks hold 256 bytes, and 16 lanes of a
+// 16-byte read, or 32 lanes of a transposing 8-byte read, are served at once:
+//   - a row read (16 lanes, 16 consecutive rows, one chunk) needs the 16 rows
+//     on 16 distinct 16-byte bank groups;
+//   - a transposing read (8 consecutive rows from a multiple of 8, two
+//     adjacent chunks) needs them on 8 distinct pairs of groups.
+// With NCH chunks per row, 16 / NCH rows fill the banks once (none left to
+// permute for NCH >= 16), so swz orders the remaining row bits such that the
+// next row bit goes to the highest chunk bit.
+#pragma once
+
+#include "common.h"
+
+namespace bcmt {
+
+// Results of the inline-assembly LDS reads below, in the pieces in which the
+// reads return them.  Nothing may touch a piece before lds_tr_wait(); take()
+// ties every piece to that wait and only then joins them, so that no register
+// copy can come before the data.
+template <typename T> struct RowRaw;
+template <> struct RowRaw<bf16> { bf16x8 v; };
+template <> struct RowRaw<float> { f32x4 a, b; };
+template <typename T> struct ColRaw;
+template <> struct ColRaw<bf16> { bf16x4 a, b; };
+template <> struct ColRaw<float> { float e[8]; };
+
+__device__ __forceinline__ bf16x8 take(RowRaw<bf16>& r) {
+  lds_tr_bind(r.v);
+  return r.v;
+}
+__device__ __forceinline__ f32x8 take(RowRaw<float>& r) {
+  lds_tr_bind(r.a);
+  lds_tr_bind(r.b);
+  return f32x8{r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]};
+}
+__device__ __forceinline__ bf16x8 take(ColRaw<bf16>& r) {
+  lds_tr_bind(r.a);
+  lds_tr_bind(r.b);
+  return bf16x8{r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]};
+}
+__device__ __forceinline__ f32x8 take(ColRaw<float>& r) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) lds_tr_bind(r.e[i]);
+  return f32x8{r.e[0], r.e[1], r.e[2], r.e[3], r.e[4], r.e[5], r.e[6], r.e[7]};
+}
+
+template <typename T, int DH>
+struct Tile {
+  static constexpr int CH = 16 / (int)sizeof(T);  // elements of a chunk
+  static constexpr int NCH = DH / CH;             // chunks of a row: 2 .. 32
+  __device__ static __forceinline__ int swz(int r) {
+    if constexpr (NCH >= 16) return ((r & 7) << 1) | ((r >> 3) & 1);
+    else if constexpr (NCH == 8) return ((r >> 3) & 1) | (r & 2) | ((r ^ (r >> 1)) & 4);
+    else if constexpr (NCH == 4) return ((r >> 1) & 2) | ((r >> 3) & 1);
+    else return (r >> 3) & 1;
+  }
+  __device__ static __forceinline__ int off(int r, int c) {
+    return r * DH + (((c / CH) ^ swz(r)) * CH) + c % CH;
+  }
+  // One wave's instruction i of the loads of a tile: 64 chunks.  Row r of the
+  // tile is row min(r0 + r, rlast) of src: a clamped row is never used
+  // unmasked.
+  __device__ static __forceinline__ void issue(const T* src, int64_t ld, int r0, int rlast, T* t,
+                                               int i, int lane) {
+    const int id = i * 64 + lane;
+    const int row = id / NCH, pos = id % NCH;
+    const int grow = min(r0 + row, rlast);
+    __builtin_amdgcn_global_load_lds(src + (int64_t)grow * ld + ((pos ^ swz(row)) * CH),
+                                     (lds_void_t*)(t + i * 64 * CH), 16, 0, 0);
+  }
+  // Row operand: elements c0 .. c0 + 7 of row r, zero from column DH on (rows
+  // narrower than a product's 32 columns).
+  __device__ static __forceinline__ RowRaw<T> row8(const T* t, int r, int c0) {
+    const int c = DH >= 32 || c0 < DH ? c0 : 0;
+    if constexpr (sizeof(T) == 2) return {lds_read_b128(t + off(r, c))};
+    else return {lds_read_f32x4(t + off(r, c)), lds_read_f32x4(t + off(r, c + 4))};
+  }
+  __device__ static __forceinline__ typename Frag<T>::type take_row(RowRaw<T>& r, int c0) {
+    typedef typename Frag<T>::type F;
+    const F f = take(r);
+    return DH >= 32 || c0 < DH ? f : F{};
+  }
+  // Column operand: column c0 + lane % 16 of rows b0 + 4g .. + 3 and
+  // b1 + 4g .. + 3, g = lane / 16: the order in which two 16-row result tiles
+  // hold their rows.
+  __device__ static __forceinline__ ColRaw<T> col8(const T* t, int b0, int b1, int c0, int lane) {
+    const int g = lane >> 4, i = lane & 15;
+    if constexpr (sizeof(T) == 2) {
+      const int rr = 4 * g + (i >> 2), cc = c0 + ((i & 3) << 2);
+      return {lds_read_tr(t + off(b0 + rr, cc)), lds_read_tr(t + off(b1 + rr, cc))};
+    } else {
+      ColRaw<T> r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        r.e[e] = lds_read_f32(t + off(b0 + 4 * g + e, c0 + i));
+        r.e[4 + e] = lds_read_f32(t + off(b1 + 4 * g + e, c0 + i));
+      }
+      return r;
+    }
+  }
+};
+
+// Workgroup barrier without the vmcnt drain of __syncthreads(): direct loads
+// stay in flight, and no memory access moves across it.
+__device__ __forceinline__ void wg_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void vm_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Sequences are rows [cu[s], cu[s + 1]) of the packed arrays, cut into tiles of
+// TILE rows from their own start.  Slot x of total / TILE + nseq slots stands
+// for tile x - first(s) of the last sequence s with first(s) <= x, where
+// first(s) = cu[s] / TILE + s: sequence s has cu[s+1] / TILE - cu[s] / TILE + 1
+// >= ceil(length / TILE) slots, and a slot behind the sequence's end is empty.
+// No host copy of cu and no table is needed.  Offsets outside [0, total] or out
+// of order are clamped, so that no row outside the arrays is ever addressed.
+// Called by whole waves; 64 sequences per search step.
+struct SeqTile {
+  int seq, begin, end, tile;  // rows [begin, end) of the sequence; tile index
+};
+__device__ __forceinline__ SeqTile find_tile(const int* __restrict__ cu, int nseq, int total,
+                                             int TILE, int slot) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = nseq;
+  while (n > 1) {
+    const int st = (n + 63) / 64;
+    const int s = lo + lane * st;
+    const bool le = lane * st < n && min(max(cu[s < lo + n ? s : lo], 0), total) / TILE + s <= slot;
+    const int c = max((int)__popcll(__ballot(le)), 1) - 1;
+    lo += c * st;
+    n = min(st, n - c * st);
+  }
+  SeqTile r;
+  r.seq = __builtin_amdgcn_readfirstlane(lo);
+  r.begin = __builtin_amdgcn_readfirstlane(min(max(cu[r.seq], 0), total));
+  r.end = __builtin_amdgcn_readfirstlane(min(max(cu[r.seq + 1], r.begin), total));
+  r.tile = slot - (r.begin / TILE + r.seq);
+  return r;
+}
+
+// Nonzero if an element is infinite or NaN (its exponent bits are all ones).
+__device__ __forceinline__ unsigned nonfinite_bits(const bf16x8& v) {
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 x = __builtin_bit_cast(u32x4, v);
+  unsigned b = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b |= ((x[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  return b;
+}
+__device__ __forceinline__ unsigned nonfinite_bits(const f32x8& v) {
+  typedef unsigned u32x8 __attribute__((ext_vector_type(8)));
+  const u32x8 x = __builtin_bit_cast(u32x8, v);
+  unsigned b = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b |= ((x[i] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+  return b;
+}
+}  // namespace bcmt
+
+// Dispatch of a launcher template over the types and head widths.
+#define BY_TYPE_AND_WIDTH(fn, dt, dh, ...)                   \
+  do {                                                       \
+    if ((dt) == DType::BF16) {                               \
+      switch (dh) {                                          \
+        case 16: return fn<bf16, 16>(__VA_ARGS__);           \
+        case 32: return fn<bf16, 32>(__VA_ARGS__);           \
+        case 64: return fn<bf16, 64>(__VA_ARGS__);           \
+        default: return fn<bf16, 128>(__VA_ARGS__);          \
+      }                                                      \
+    }                                                        \
+    switch (dh) {                                            \
+      case 16: return fn<float, 16>(__VA_ARGS__);            \
+      case 32: return fn<float, 32>(__VA_ARGS__);            \
+      case 64: return fn<float, 64>(__VA_ARGS__);            \
+      default: return fn<float, 128>(__VA_ARGS__);           \
+    }                                                        \
+  } while (0)
+

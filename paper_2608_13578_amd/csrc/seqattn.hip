@@ -1,0 +1,833 @@
+// Causal softmax attention over packed sequences with grouped heads.
+//
+// Rows [cu[s], cu[s+1]) of the packed arrays are sequence s.  Query head h
+// reads key/value head j = h / G.  For a row t and the rows u <= t of its
+// sequence:
+//   z_tu = scale q_t . k_u,  p_tu = exp(z_tu - lse_t),  lse_t = log sum_u exp z_tu
+//   o_t = sum_u p_tu v_u
+//   delta_t = do_t . o_t,  dz_tu = p_tu (do_t . v_u - delta_t)
+//   dq_t = scale sum_u dz_tu k_u
+//   dk_u = scale sum_h sum_t dz_tu q_t,  dv_u = sum_h sum_t p_tu do_t
+// with the sums over h taken over the group of query heads.  No score matrix
+// leaves registers.
+//
+// Register layouts (common.h): a matrix instruction returns lane l the column
+// l % 16 and rows 4 (l / 16) + r.  The forward and dQ compute transposed
+// scores, so a lane holds one query and a set of keys, and those registers are
+// the second operand of the next product as they are (Tile::col8 reads the
+// first operand in the same key order).  dK/dV computes them untransposed,
+// one key per lane, to the same end.
+#include "kernels.h"
+#include "mixer_tile.h"
+
+namespace bcmt {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type gfrag(const T* p, bool ok) {
+  typedef typename Frag<T>::type F;
+  return ok ? load_frag(p) : F{};
+}
+
+// The two tiles (K, V or Q, dO) of one step, 2 NCH wave instructions shared by
+// NW waves.
+template <typename T, int DH, int NW>
+__device__ __forceinline__ void issue_pair(const T* a, int64_t lda, const T* b, int64_t ldb, int r0,
+                                           int rlast, T* ta, T* tb, int wave, int lane) {
+  typedef Tile<T, DH> TL;
+  constexpr int NI = 2 * TL::NCH / NW;
+  static_assert(NI >= 1 && NI * NW == 2 * TL::NCH, "loads of two tiles");
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int gi = wave * NI + i;
+    if (gi < TL::NCH) TL::issue(a, lda, r0, rlast, ta, gi, lane);
+    else TL::issue(b, ldb, r0, rlast, tb, gi - TL::NCH, lane);
+  }
+}
+
+// ------------------------------------------------------------------ forward
+// One workgroup of four waves: 64 NQ queries of one head, NQ groups of 16 per
+// wave.  Tiles of 64 keys, double buffered; running maximum and sum.
+
+template <typename T, int DH, int NQ>
+__global__ __launch_bounds__(256) void seq_fwd_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+    const int* __restrict__ cu, T* __restrict__ o, float* __restrict__ lse, int total, int nseq,
+    int H, int G, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2) {
+  typedef typename Frag<T>::type F;
+  typedef Tile<T, DH> TL;
+  constexpr int NW = 4, QT = NW * 16 * NQ, KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
+  constexpr int NI = 2 * TL::NCH / NW;
+  constexpr int KUS = sizeof(T) == 2 ? 4 : 1;  // key groups whose fragments are live at once
+  __shared__ __attribute__((aligned(1024))) T lds[2][2][64 * DH];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lr = lane & 15, lg = lane >> 4;
+  const int nslot = total / QT + nseq;
+  const int h = blockIdx.x % H;
+  const SeqTile st = find_tile(cu, nseq, total, QT, nslot - 1 - (int)(blockIdx.x / H));
+  const int bs = st.begin, be = st.end, q0 = bs + st.tile * QT;
+  if (st.tile < 0 || q0 >= be) return;
+  const int j = h / G;
+  const T* kb = k + j * DH;
+  const T* vb = v + j * DH;
+  // Groups of 16 queries are dealt w, 2 NW - 1 - w: a causal group's work grows
+  // with its position.
+  int tq[NQ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) tq[nq] = q0 + 16 * (nq & 1 ? 2 * NW - 1 - wave : wave);
+  const int kend = min(be, q0 + QT);
+  const int nt = (kend - bs + 63) / 64;
+
+  F qf[NQ][KS];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) {
+      const int t = tq[nq] + lr, c = ds * 32 + lg * 8;
+      qf[nq][ds] = gfrag(q + (int64_t)t * ldq + h * DH + c, t < be && c < DH);
+    }
+  f32x4 oa[NQ][NJ];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    m[nq] = -INFINITY;
+    l[nq] = 0.f;
+#pragma unroll
+    for (int jj = 0; jj < NJ; ++jj) oa[nq][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs, kend - 1, lds[0][0], lds[0][1], wave, lane);
+  if (nt > 1)
+    issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + 64, kend - 1, lds[1][0], lds[1][1], wave, lane);
+  for (int it = 0; it < nt; ++it) {
+    if (it + 1 < nt) vm_wait<NI>();
+    else vm_wait<0>();
+    wg_barrier();
+    const int kt = bs + it * 64;
+    const T* Kt = lds[it & 1][0];
+    const T* Vt = lds[it & 1][1];
+    bool live[NQ], any = false;
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+      live[nq] = !(tq[nq] >= be || tq[nq] + 15 < kt);  // wave-uniform
+      any |= live[nq];
+    }
+    if (any) {
+      f32x4 s[NQ][4];
+#pragma unroll
+      for (int k0 = 0; k0 < 4; k0 += KUS) {
+        RowRaw<T> kr[KUS][KS];
+#pragma unroll
+        for (int ku = 0; ku < KUS; ++ku)
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds)
+            kr[ku][ds] = TL::row8(Kt, (k0 + ku) * 16 + lr, ds * 32 + lg * 8);
+        lds_tr_wait();
+#pragma unroll
+        for (int ku = 0; ku < KUS; ++ku) {
+          F kf[KS];
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) kf[ds] = TL::take_row(kr[ku][ds], ds * 32 + lg * 8);
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq) {
+            s[nq][k0 + ku] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ds = 0; ds < KS; ++ds)
+              s[nq][k0 + ku] = mma16(kf[ds], qf[nq][ds], s[nq][k0 + ku]);
+          }
+        }
+      }
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        if (!live[nq]) continue;
+        const int t_eff = min(tq[nq] + lr, be - 1);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int ku = 0; ku < 4; ++ku)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int u = kt + ku * 16 + lg * 4 + r;
+            const float z = u <= t_eff ? s[nq][ku][r] * sl2 : -INFINITY;
+            s[nq][ku][r] = z;
+            mx = fmaxf(mx, z);
+          }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float mnew = fmaxf(m[nq], mx);
+        // all scores so far -inf: subtract 0, so that the weights are 0 and
+        // later finite scores still count
+        const float ms = mnew == -INFINITY ? 0.f : mnew;
+        const float alpha = exp2_fast(m[nq] - ms);
+        float ps = 0.f;
+#pragma unroll
+        for (int ku = 0; ku < 4; ++ku)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float p = exp2_fast(s[nq][ku][r] - ms);
+            s[nq][ku][r] = p;
+            ps += p;
+          }
+        l[nq] = l[nq] * alpha + ps;
+        m[nq] = mnew;
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) oa[nq][jj] *= alpha;
+      }
+      // A value that is not finite, in a row that some query of the tile does
+      // not see: 0 * inf would reach that query through the products.  Such a
+      // half tile is summed key by key over the visible rows instead.
+#pragma unroll
+      for (int us = 0; us < 2; ++us) {
+        ColRaw<T> vr[NJ];
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) vr[jj] = TL::col8(Vt, us * 32, us * 32 + 16, jj * 16, lane);
+        lds_tr_wait();
+        F vf[NJ];
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) vf[jj] = take(vr[jj]);
+        bool slow = false;
+        if (kt + us * 32 + 31 > q0) {
+          unsigned bad = 0;
+#pragma unroll
+          for (int jj = 0; jj < NJ; ++jj) bad |= nonfinite_bits(vf[jj]);
+          slow = __ballot(bad != 0) != 0;
+        }
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+          if (!live[nq]) continue;
+          if (!slow) {
+            const F pf = frag_from<T>(s[nq][2 * us], s[nq][2 * us + 1]);
+#pragma unroll
+            for (int jj = 0; jj < NJ; ++jj) oa[nq][jj] = mma16(vf[jj], pf, oa[nq][jj]);
+            continue;
+          }
+          const int t_eff = min(tq[nq] + lr, be - 1);
+#pragma unroll 1
+          for (int gg = 0; gg < 4; ++gg)
+#pragma unroll
+            for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const int ui = us * 32 + k2 * 16 + gg * 4 + r;
+                const float p =
+                    to_f32(from_f32<T>(__shfl(s[nq][2 * us + k2][r], lr + 16 * gg, 64)));
+                if (kt + ui > t_eff) continue;
+#pragma unroll
+                for (int jj = 0; jj < NJ; ++jj) {
+                  const f32x4 vv = load4f(Vt + TL::off(ui, jj * 16 + lg * 4));
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) oa[nq][jj][e] = fmaf(p, vv[e], oa[nq][jj][e]);
+                }
+              }
+        }
+      }
+    }
+    if (it + 2 < nt) {
+      wg_barrier();  // every wave is done with this buffer
+      issue_pair<T, DH, NW>(kb, ldk, vb, ldv, kt + 128, kend - 1, lds[it & 1][0], lds[it & 1][1],
+                            wave, lane);
+    }
+  }
+
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    float lt = l[nq];
+    lt += __shfl_xor(lt, 16, 64);
+    lt += __shfl_xor(lt, 32, 64);
+    const int t = tq[nq] + lr;
+    if (t < be) {
+      const float inv = 1.0f / lt;
+      T* op = o + (int64_t)t * ldo + h * DH + lg * 4;
+#pragma unroll
+      for (int jj = 0; jj < NJ; ++jj)
+        store4(op + jj * 16, oa[nq][jj][0] * inv, oa[nq][jj][1] * inv, oa[nq][jj][2] * inv,
+               oa[nq][jj][3] * inv);
+      if (lse && lg == 0) lse[(int64_t)h * total + t] = m[nq] * kLn2 + logf(lt);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ backward: dQ
+// The forward's walk again, with delta_t = do_t . o_t formed (and stored for
+// dK/dV) first: s and dp per key tile, dz in place, dQ^T += K^T dZ^T.
+
+template <typename T, int DH, int NQ>
+__global__ __launch_bounds__(256) void seq_dq_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+    const int* __restrict__ cu, const T* __restrict__ o, const float* __restrict__ lse,
+    const T* __restrict__ dout, T* __restrict__ dq, float* __restrict__ delta, int total, int nseq,
+    int H, int G, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2, float scale) {
+  typedef typename Frag<T>::type F;
+  typedef Tile<T, DH> TL;
+  constexpr int NW = 4, QT = NW * 16 * NQ, KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
+  constexpr int NI = 2 * TL::NCH / NW;
+  __shared__ __attribute__((aligned(1024))) T lds[2][2][64 * DH];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lr = lane & 15, lg = lane >> 4;
+  const int nslot = total / QT + nseq;
+  const int h = blockIdx.x % H;
+  const SeqTile st = find_tile(cu, nseq, total, QT, nslot - 1 - (int)(blockIdx.x / H));
+  const int bs = st.begin, be = st.end, q0 = bs + st.tile * QT;
+  if (st.tile < 0 || q0 >= be) return;
+  const int j = h / G;
+  const T* kb = k + j * DH;
+  const T* vb = v + j * DH;
+  int tq[NQ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) tq[nq] = q0 + 16 * (nq & 1 ? 2 * NW - 1 - wave : wave);
+  const int kend = min(be, q0 + QT);
+  const int nt = (kend - bs + 63) / 64;
+
+  F qf[NQ][KS], df[NQ][KS];
+  float dl[NQ], ls[NQ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    const int t = tq[nq] + lr;
+    float part = 0.f;
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) {
+      const int c = ds * 32 + lg * 8;
+      const bool ok = t < be && c < DH;
+      qf[nq][ds] = gfrag(q + (int64_t)t * ldq + h * DH + c, ok);
+      df[nq][ds] = gfrag(dout + (int64_t)t * ldo + h * DH + c, ok);
+      const F of = gfrag(o + (int64_t)t * ldo + h * DH + c, ok);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) part += to_f32(df[nq][ds][e]) * to_f32(of[e]);
+    }
+    part += __shfl_xor(part, 16, 64);
+    part += __shfl_xor(part, 32, 64);
+    dl[nq] = part;
+    ls[nq] = t < be ? lse[(int64_t)h * total + t] * kLog2e : 0.f;
+    if (t < be && lg == 0) delta[(int64_t)h * total + t] = part;
+  }
+  f32x4 da[NQ][NJ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+    for (int jj = 0; jj < NJ; ++jj) da[nq][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs, kend - 1, lds[0][0], lds[0][1], wave, lane);
+  if (nt > 1)
+    issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + 64, kend - 1, lds[1][0], lds[1][1], wave, lane);
+  for (int it = 0; it < nt; ++it) {
+    if (it + 1 < nt) vm_wait<NI>();
+    else vm_wait<0>();
+    wg_barrier();
+    const int kt = bs + it * 64;
+    const T* Kt = lds[it & 1][0];
+    const T* Vt = lds[it & 1][1];
+    bool live[NQ], any = false;
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+      live[nq] = !(tq[nq] >= be || tq[nq] + 15 < kt);  // wave-uniform
+      any |= live[nq];
+    }
+    if (any) {
+      // 32 keys at a time: scores and dp of two key groups, then their part of dQ
+#pragma unroll
+      for (int us = 0; us < 2; ++us) {
+        f32x4 s[NQ][2];
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          const int ku = us * 2 + k2;
+          RowRaw<T> kr[KS], vr[KS];
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) {
+            kr[ds] = TL::row8(Kt, ku * 16 + lr, ds * 32 + lg * 8);
+            vr[ds] = TL::row8(Vt, ku * 16 + lr, ds * 32 + lg * 8);
+          }
+          lds_tr_wait();
+          F kf[KS], vf[KS];
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) {
+            kf[ds] = TL::take_row(kr[ds], ds * 32 + lg * 8);
+            vf[ds] = TL::take_row(vr[ds], ds * 32 + lg * 8);
+          }
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq) {
+            f32x4 sv = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ds = 0; ds < KS; ++ds) {
+              sv = mma16(kf[ds], qf[nq][ds], sv);
+              dp = mma16(vf[ds], df[nq][ds], dp);
+            }
+            const int t_eff = min(tq[nq] + lr, be - 1);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int u = kt + ku * 16 + lg * 4 + r;
+              s[nq][k2][r] =
+                  u <= t_eff ? exp2_fast(sv[r] * sl2 - ls[nq]) * (dp[r] - dl[nq]) : 0.f;
+            }
+          }
+        }
+        F zf[NQ];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) zf[nq] = frag_from<T>(s[nq][0], s[nq][1]);
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) {
+          ColRaw<T> kr = TL::col8(Kt, us * 32, us * 32 + 16, jj * 16, lane);
+          lds_tr_wait();
+          const F kc = take(kr);
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq)
+            if (live[nq]) da[nq][jj] = mma16(kc, zf[nq], da[nq][jj]);
+        }
+      }
+    }
+    if (it + 2 < nt) {
+      wg_barrier();
+      issue_pair<T, DH, NW>(kb, ldk, vb, ldv, kt + 128, kend - 1, lds[it & 1][0], lds[it & 1][1],
+                            wave, lane);
+    }
+  }
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    const int t = tq[nq] + lr;
+    if (t < be) {
+      T* p = dq + (int64_t)t * ldq + h * DH + lg * 4;
+#pragma unroll
+      for (int jj = 0; jj < NJ; ++jj)
+        store4(p + jj * 16, da[nq][jj][0] * scale, da[nq][jj][1] * scale, da[nq][jj][2] * scale,
+               da[nq][jj][3] * scale);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ backward: dK, dV
+// One workgroup of four waves: 64 NK keys of one key/value head, NK groups of
+// 16 per wave.  It walks the query tiles at or after its keys, for every query
+// head of the group in turn, so that shared heads are summed in registers in
+// a fixed order.
+
+template <typename T, int DH, int NK>
+__global__ __launch_bounds__(256) void seq_dkdv_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+    const int* __restrict__ cu, const float* __restrict__ lse, const float* __restrict__ delta,
+    const T* __restrict__ dout, T* __restrict__ dk, T* __restrict__ dv, int total, int nseq, int H,
+    int G, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2, float scale) {
+  typedef typename Frag<T>::type F;
+  typedef Tile<T, DH> TL;
+  constexpr int NW = 4, KT = NW * 16 * NK, KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
+  constexpr int NI = 2 * TL::NCH / NW + 1;
+  __shared__ __attribute__((aligned(1024))) T lds[2][2][64 * DH];
+  __shared__ __attribute__((aligned(16))) float rows[2][NW][64];  // lse, delta: waves 0 and 1
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lr = lane & 15, lg = lane >> 4;
+  const int Hkv = H / G;
+  const int j = blockIdx.x % Hkv;
+  const SeqTile st = find_tile(cu, nseq, total, KT, (int)(blockIdx.x / Hkv));
+  const int be = st.end, k0 = st.begin + st.tile * KT;
+  if (st.tile < 0 || k0 >= be) return;
+  const int nt1 = (be - k0 + 63) / 64, nt = nt1 * G;  // query tiles of a head, of all
+
+  int uk[NK];
+  F kf[NK][KS], vf[NK][KS];
+  f32x4 ka[NK][NJ], va[NK][NJ];
+#pragma unroll
+  for (int nk = 0; nk < NK; ++nk) {
+    uk[nk] = k0 + 16 * (nk & 1 ? 2 * NW - 1 - wave : wave);
+    const int u = uk[nk] + lr;
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) {
+      const int c = ds * 32 + lg * 8;
+      kf[nk][ds] = gfrag(k + (int64_t)u * ldk + j * DH + c, u < be && c < DH);
+      vf[nk][ds] = gfrag(v + (int64_t)u * ldv + j * DH + c, u < be && c < DH);
+    }
+#pragma unroll
+    for (int jj = 0; jj < NJ; ++jj) {
+      ka[nk][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+      va[nk][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  auto issue = [&](int it) {
+    const int h = j * G + it / nt1, tt = k0 + (it % nt1) * 64;
+    issue_pair<T, DH, NW>(q + h * DH, ldq, dout + h * DH, ldo, tt, be - 1, lds[it & 1][0],
+                          lds[it & 1][1], wave, lane);
+    const float* src = (wave & 1 ? delta : lse) + (int64_t)h * total + min(tt + lane, be - 1);
+    __builtin_amdgcn_global_load_lds(src, (lds_void_t*)rows[it & 1][wave], 4, 0, 0);
+  };
+
+  issue(0);
+  if (nt > 1) issue(1);
+  for (int it = 0; it < nt; ++it) {
+    if (it + 1 < nt) vm_wait<NI>();
+    else vm_wait<0>();
+    wg_barrier();
+    const int tt = k0 + (it % nt1) * 64;
+    const T* Qt = lds[it & 1][0];
+    const T* Dt = lds[it & 1][1];
+    bool live[NK], any = false;
+#pragma unroll
+    for (int nk = 0; nk < NK; ++nk) {
+      live[nk] = !(uk[nk] >= be || tt + 63 < uk[nk]);  // wave-uniform
+      any |= live[nk];
+    }
+    if (any) {
+      // 32 queries at a time
+#pragma unroll
+      for (int us = 0; us < 2; ++us) {
+        f32x4 p[NK][2], z[NK][2];
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2) {
+          const int ts = us * 2 + t2;
+          RowRaw<T> qr[KS], dr[KS];
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) {
+            qr[ds] = TL::row8(Qt, ts * 16 + lr, ds * 32 + lg * 8);
+            dr[ds] = TL::row8(Dt, ts * 16 + lr, ds * 32 + lg * 8);
+          }
+          f32x4 ls = lds_read_f32x4(&rows[it & 1][0][ts * 16 + lg * 4]);
+          f32x4 dl = lds_read_f32x4(&rows[it & 1][1][ts * 16 + lg * 4]);
+          lds_tr_wait();
+          F qf[KS], df[KS];
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) {
+            qf[ds] = TL::take_row(qr[ds], ds * 32 + lg * 8);
+            df[ds] = TL::take_row(dr[ds], ds * 32 + lg * 8);
+          }
+          lds_tr_bind(ls);
+          lds_tr_bind(dl);
+#pragma unroll
+          for (int nk = 0; nk < NK; ++nk) {
+            f32x4 sv = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ds = 0; ds < KS; ++ds) {
+              sv = mma16(qf[ds], kf[nk][ds], sv);
+              dp = mma16(df[ds], vf[nk][ds], dp);
+            }
+            const int u = uk[nk] + lr;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int t = tt + ts * 16 + lg * 4 + r;
+              const bool ok = t >= u && t < be;
+              const float pv = ok ? exp2_fast(sv[r] * sl2 - ls[r] * kLog2e) : 0.f;
+              p[nk][t2][r] = pv;
+              z[nk][t2][r] = ok ? pv * (dp[r] - dl[r]) : 0.f;
+            }
+          }
+        }
+        F pf[NK], zf[NK];
+#pragma unroll
+        for (int nk = 0; nk < NK; ++nk) {
+          pf[nk] = frag_from<T>(p[nk][0], p[nk][1]);
+          zf[nk] = frag_from<T>(z[nk][0], z[nk][1]);
+        }
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) {
+          ColRaw<T> dr = TL::col8(Dt, us * 32, us * 32 + 16, jj * 16, lane);
+          ColRaw<T> qr = TL::col8(Qt, us * 32, us * 32 + 16, jj * 16, lane);
+          lds_tr_wait();
+          const F dc = take(dr), qc = take(qr);
+#pragma unroll
+          for (int nk = 0; nk < NK; ++nk)
+            if (live[nk]) {
+              va[nk][jj] = mma16(dc, pf[nk], va[nk][jj]);
+              ka[nk][jj] = mma16(qc, zf[nk], ka[nk][jj]);
+            }
+        }
+      }
+    }
+    if (it + 2 < nt) {
+      wg_barrier();
+      issue(it + 2);
+    }
+  }
+#pragma unroll
+  for (int nk = 0; nk < NK; ++nk) {
+    const int u = uk[nk] + lr;
+    if (u < be) {
+      T* pk = dk + (int64_t)u * ldk + j * DH + lg * 4;
+      T* pv = dv + (int64_t)u * ldv + j * DH + lg * 4;
+#pragma unroll
+      for (int jj = 0; jj < NJ; ++jj) {
+        store4(pk + jj * 16, ka[nk][jj][0] * scale, ka[nk][jj][1] * scale, ka[nk][jj][2] * scale,
+               ka[nk][jj][3] * scale);
+        store4(pv + jj * 16, va[nk][jj][0], va[nk][jj][1], va[nk][jj][2], va[nk][jj][3]);
+      }
+    }
+  }
+}
+
+template <typename T, int DH>
+hipError_t fwd_t(const SeqAttn& a, hipStream_t s) {
+  constexpr int NQ = sizeof(T) == 2 ? 2 : 1, QT = 64 * NQ;
+  const int64_t grid = (int64_t)(a.total / QT + a.nseq) * a.H;
+  seq_fwd_kernel<T, DH, NQ><<<dim3((unsigned)grid), 256, 0, s>>>(
+      (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, (T*)a.o, a.lse, a.total, a.nseq, a.H,
+      a.H / a.Hkv, a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e);
+  return hipGetLastError();
+}
+
+template <typename T, int DH>
+hipError_t bwd_t(const SeqAttn& a, hipStream_t s) {
+  constexpr int NQ = sizeof(T) == 2 ? 2 : 1, QT = 64 * NQ;
+  const int G = a.H / a.Hkv;
+  const int64_t gq = (int64_t)(a.total / QT + a.nseq) * a.H;
+  seq_dq_kernel<T, DH, NQ><<<dim3((unsigned)gq), 256, 0, s>>>(
+      (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, (const T*)a.o, a.lse, (const T*)a.dout,
+      (T*)a.dq, a.delta, a.total, a.nseq, a.H, G, a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e,
+      a.scale);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t gk = (int64_t)(a.total / QT + a.nseq) * a.Hkv;
+  seq_dkdv_kernel<T, DH, NQ><<<dim3((unsigned)gk), 256, 0, s>>>(
+      (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, a.lse, a.delta, (const T*)a.dout,
+      (T*)a.dk, (T*)a.dv, a.total, a.nseq, a.H, G, a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e,
+      a.scale);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ single tokens
+// One workgroup per (sequence, key/value head, 16 query heads of its group,
+// part of the cache).  The heads of the group are the columns of the score
+// product, so each cache row is read once for all of them.  Every wave walks
+// its own tiles of KT keys through its own LDS (no barriers), and the waves'
+// maxima, sums and outputs are joined at the end.  The token's own key and
+// value are put into the tile that holds its position, whose later rows are
+// cleared (the cache may hold anything there); the wave that owns the tile
+// also writes them to the cache.
+
+template <typename T, int DH> struct DecShape {
+  // LDS of two buffers of K and V tiles per wave
+  static constexpr int KT = 32;
+  static constexpr int NW = (int)sizeof(T) * DH >= 512 ? 2 : 4;
+};
+
+template <typename T, int DH>
+__global__ __launch_bounds__((DecShape<T, DH>::NW * 64)) void dec_part_kernel(DecAttn a) {
+  typedef typename Frag<T>::type F;
+  typedef Tile<T, DH> TL;
+  constexpr int KT = DecShape<T, DH>::KT, NW = DecShape<T, DH>::NW;
+  constexpr int KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
+  constexpr int NI = KT * TL::NCH / 64;  // loads of a tile
+  static_assert(NI >= 1 && NI * 64 == KT * TL::NCH, "tile loads");
+  __shared__ __attribute__((aligned(1024))) T lds[NW][2][2][KT * DH];
+  __shared__ float red_m[NW][16], red_l[NW][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lr = lane & 15, lg = lane >> 4;
+  const int G = a.H / a.Hkv, NH = (G + 15) / 16;
+  const int part = blockIdx.x, y = blockIdx.y;
+  const int hg = y % NH, j = (y / NH) % a.Hkv, b = y / NH / a.Hkv;
+  const int slot = a.slot ? a.slot[b] : b, n = a.length[b];
+  const int h = j * G + hg * 16 + lr;      // this lane's query head
+  const bool hok = hg * 16 + lr < G;
+  if (slot < 0 || slot >= a.slots || n < 0 || n >= a.cap) {
+    if (part == 0 && a.nsplit == 1 && wave == 0 && hok)
+      for (int jj = 0; jj < NJ; ++jj)
+        store4((T*)a.o + (int64_t)b * a.ldo + h * DH + jj * 16 + lg * 4, 0.f, 0.f, 0.f, 0.f);
+    return;
+  }
+  const int ntile = n / KT + 1;  // rows 0 .. n
+  const int per = (ntile + a.nsplit - 1) / a.nsplit;
+  const int t0 = part * per, t1 = min(t0 + per, ntile);
+  if (t0 >= t1) return;
+  T* kc = (T*)a.kcache + slot * a.cs + j * a.ch;
+  T* vc = (T*)a.vcache + slot * a.cs + j * a.ch;
+  const T* kn = (const T*)a.k + (int64_t)b * a.ldk + j * DH;
+  const T* vn = (const T*)a.v + (int64_t)b * a.ldv + j * DH;
+
+  F qf[KS];
+#pragma unroll
+  for (int ds = 0; ds < KS; ++ds) {
+    const int c = ds * 32 + lg * 8;
+    qf[ds] = gfrag((const T*)a.q + (int64_t)b * a.ldq + h * DH + c, hok && c < DH);
+  }
+  float m = -INFINITY, l = 0.f;
+  f32x4 oa[NJ];
+#pragma unroll
+  for (int jj = 0; jj < NJ; ++jj) oa[jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  auto issue = [&](int t, int buf) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) TL::issue(kc, a.ct, t * KT, n, lds[wave][buf][0], i, lane);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) TL::issue(vc, a.ct, t * KT, n, lds[wave][buf][1], i, lane);
+  };
+  int t = t0 + wave, buf = 0;
+  if (t < t1) issue(t, 0);
+  if (t + NW < t1) issue(t + NW, 1);
+  for (; t < t1; t += NW, buf ^= 1) {
+    if (t + NW < t1) vm_wait<2 * NI>();
+    else vm_wait<0>();
+    T* Kt = lds[wave][buf][0];
+    T* Vt = lds[wave][buf][1];
+    if (t * KT + KT > n) {  // the tile of position n
+      for (int id = lane; id < KT * TL::NCH; id += 64) {
+        const int r = id / TL::NCH, c = (id % TL::NCH) * TL::CH, u = t * KT + r;
+        if (u < n) continue;
+        typename Vec16<T>::type kv = {}, vv = {};
+        if (u == n) {
+          kv = load16(kn + c);
+          vv = load16(vn + c);
+          if (hg == 0) {
+            store16(kc + (int64_t)n * a.ct + c, kv);
+            store16(vc + (int64_t)n * a.ct + c, vv);
+          }
+        }
+        store16(Kt + TL::off(r, c), kv);
+        store16(Vt + TL::off(r, c), vv);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    f32x4 s[2];
+    ColRaw<T> vr[NJ];
+#pragma unroll
+    for (int ku = 0; ku < 2; ++ku) {
+      RowRaw<T> kr[KS];
+#pragma unroll
+      for (int ds = 0; ds < KS; ++ds) kr[ds] = TL::row8(Kt, ku * 16 + lr, ds * 32 + lg * 8);
+      lds_tr_wait();
+      s[ku] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ds = 0; ds < KS; ++ds)
+        s[ku] = mma16(TL::take_row(kr[ds], ds * 32 + lg * 8), qf[ds], s[ku]);
+    }
+#pragma unroll
+    for (int jj = 0; jj < NJ; ++jj) vr[jj] = TL::col8(Vt, 0, 16, jj * 16, lane);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int ku = 0; ku < 2; ++ku)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int u = t * KT + ku * 16 + lg * 4 + r;
+        s[ku][r] = u <= n ? s[ku][r] * a.sl2 : -INFINITY;
+        mx = fmaxf(mx, s[ku][r]);
+      }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float mnew = fmaxf(m, mx);
+    const float ms = mnew == -INFINITY ? 0.f : mnew;
+    const float alpha = exp2_fast(m - ms);
+    float ps = 0.f;
+#pragma unroll
+    for (int ku = 0; ku < 2; ++ku)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[ku][r] = exp2_fast(s[ku][r] - ms);
+        ps += s[ku][r];
+      }
+    l = l * alpha + ps;
+    m = mnew;
+    const F pf = frag_from<T>(s[0], s[1]);
+    lds_tr_wait();
+#pragma unroll
+    for (int jj = 0; jj < NJ; ++jj) oa[jj] = mma16(take(vr[jj]), pf, oa[jj] * alpha);
+    if (t + 2 * NW < t1) issue(t + 2 * NW, buf);
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+
+  // join the waves: the weights of each wave's maximum, then the outputs
+  // through the first wave's own tiles (every wave is past its loop)
+  if (lg == 0) {
+    red_m[wave][lr] = m;
+    red_l[wave][lr] = l;
+  }
+  __syncthreads();
+  float mm = -INFINITY, lt = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) mm = fmaxf(mm, red_m[w][lr]);
+  const float msafe = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) lt += red_l[w][lr] * exp2_fast(red_m[w][lr] - msafe);
+  const float wgt = exp2_fast(m - msafe);
+  float* acc = (float*)&lds[0][0][0][0];  // [NW][16][DH] floats
+  static_assert((size_t)NW * 16 * DH * 4 <= sizeof(T) * NW * 4 * KT * DH, "join buffer");
+#pragma unroll
+  for (int jj = 0; jj < NJ; ++jj)
+    store4(acc + (wave * 16 + lr) * DH + jj * 16 + lg * 4, oa[jj][0] * wgt, oa[jj][1] * wgt,
+           oa[jj][2] * wgt, oa[jj][3] * wgt);
+  __syncthreads();
+  if (wave == 0 && lg == 0) {
+    red_m[0][lr] = mm;
+    red_l[0][lr] = lt;
+  }
+  __syncthreads();
+  const int heads = min(16, G - hg * 16);
+  for (int i = threadIdx.x; i < heads * (DH / 4); i += NW * 64) {
+    const int hh = i / (DH / 4), c = (i % (DH / 4)) * 4;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) v += *(const f32x4*)(acc + (w * 16 + hh) * DH + c);
+    const int head = j * G + hg * 16 + hh;
+    if (a.nsplit == 1) {
+      const float inv = 1.0f / red_l[0][hh];
+      store4((T*)a.o + (int64_t)b * a.ldo + head * DH + c, v[0] * inv, v[1] * inv, v[2] * inv,
+             v[3] * inv);
+    } else {
+      const int64_t row = ((int64_t)b * a.H + head) * a.nsplit + part;
+      *(f32x4*)(a.part_o + row * DH + c) = v;
+      if (c == 0) {
+        a.part_ml[row * 2] = red_m[0][hh];
+        a.part_ml[row * 2 + 1] = red_l[0][hh];
+      }
+    }
+  }
+}
+
+// Joins the parts of one (sequence, head): DH / 4 lanes each.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void dec_join_kernel(DecAttn a) {
+  constexpr int KT = DecShape<T, DH>::KT, PER = 256 / (DH / 4);
+  const int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / (DH / 4);
+  if (row >= (int64_t)a.B * a.H) return;
+  const int b = (int)(row / a.H), h = (int)(row % a.H), c = (threadIdx.x % (DH / 4)) * 4;
+  const int slot = a.slot ? a.slot[b] : b, n = a.length[b];
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float inv = 0.f;
+  if (slot >= 0 && slot < a.slots && n >= 0 && n < a.cap) {
+    const int ntile = n / KT + 1, per = (ntile + a.nsplit - 1) / a.nsplit;
+    const int np = (ntile + per - 1) / per;
+    const float* ml = a.part_ml + row * a.nsplit * 2;
+    float m = -INFINITY, l = 0.f;
+    for (int p = 0; p < np; ++p) m = fmaxf(m, ml[2 * p]);
+    const float ms = m == -INFINITY ? 0.f : m;
+    for (int p = 0; p < np; ++p) {
+      const float w = exp2_fast(ml[2 * p] - ms);
+      l += w * ml[2 * p + 1];
+      acc += w * *(const f32x4*)(a.part_o + (row * a.nsplit + p) * DH + c);
+    }
+    inv = 1.0f / l;
+  }
+  store4((T*)a.o + (int64_t)b * a.ldo + h * DH + c, acc[0] * inv, acc[1] * inv, acc[2] * inv,
+         acc[3] * inv);
+}
+
+template <typename T, int DH>
+hipError_t dec_t(const DecAttn& a, hipStream_t s) {
+  constexpr int NW = DecShape<T, DH>::NW;
+  const int G = a.H / a.Hkv, NH = (G + 15) / 16;
+  dec_part_kernel<T, DH><<<dim3(a.nsplit, a.B * a.Hkv * NH), NW * 64, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.nsplit == 1) return e;
+  constexpr int PER = 256 / (DH / 4);
+  dec_join_kernel<T, DH><<<dim3((unsigned)(((int64_t)a.B * a.H + PER - 1) / PER)), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t seq_attn_fwd(DType dt, int dh, const SeqAttn& a, hipStream_t s) {
+  BY_TYPE_AND_WIDTH(fwd_t, dt, dh, a, s);
+}
+hipError_t seq_attn_bwd(DType dt, int dh, const SeqAttn& a, hipStream_t s) {
+  BY_TYPE_AND_WIDTH(bwd_t, dt, dh, a, s);
+}
+hipError_t seq_attn_decode(DType dt, int dh, const DecAttn& a, hipStream_t s) {
+  BY_TYPE_AND_WIDTH(dec_t, dt, dh, a, s);
+}
+
+// Parts of the cache: enough workgroups for four per CU, at least two tiles of
+// every wave in a part.
+int seq_attn_decode_splits(DType dt, int dh, int B, int H, int Hkv, int cap) {
+  const int G = H / Hkv, NH = (G + 15) / 16;
+  const int nw = (dt == DType::BF16 ? 2 : 4) * dh >= 512 ? 2 : 4;
+  const int64_t wgs = (int64_t)B * Hkv * NH;
+  const int64_t want = (1024 + wgs - 1) / wgs, most = (cap + nw * 64 - 1) / (nw * 64);
+  const int64_t n = want < most ? want : most;
+  return n < 1 ? 1 : (int)n;
+}
+
+}  // namespace bcmt
