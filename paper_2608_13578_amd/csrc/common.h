@@ -250,13 +250,6 @@ __device__ __forceinline__ bf16x8 lds_read_b128(const bf16* p) {
   asm volatile("ds_read_b128 %0, %1" : "=v"(v) : "v"(a));
   return v;
 }
-// 8-byte bf16 LDS read in inline assembly; same contract as lds_read_tr().
-__device__ __forceinline__ bf16x4 lds_read_b64(const bf16* p) {
-  bf16x4 v;
-  const unsigned a = (unsigned)(uintptr_t)((__attribute__((address_space(3))) bf16*)(p));
-  asm volatile("ds_read_b64 %0, %1" : "=v"(v) : "v"(a));
-  return v;
-}
 // The same reads at a byte address plus an immediate offset.
 template <int OFF>
 __device__ __forceinline__ bf16x4 lds_read_tr_at(unsigned a) {
@@ -268,6 +261,24 @@ template <int OFF>
 __device__ __forceinline__ bf16x8 lds_read_b128_at(unsigned a) {
   bf16x8 v;
   asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(a), "n"(OFF));
+  return v;
+}
+template <int OFF>
+__device__ __forceinline__ bf16x4 lds_read_b64_at(unsigned a) {
+  bf16x4 v;
+  asm volatile("ds_read_b64 %0, %1 offset:%2" : "=v"(v) : "v"(a), "n"(OFF));
+  return v;
+}
+template <int OFF>
+__device__ __forceinline__ f32x4 lds_read_f32x4_at(unsigned a) {
+  f32x4 v;
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(a), "n"(OFF));
+  return v;
+}
+template <int OFF>
+__device__ __forceinline__ float lds_read_f32_at(unsigned a) {
+  float v;
+  asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(a), "n"(OFF));
   return v;
 }
 // Waits for every outstanding LDS read of this wave.

@@ -70,11 +70,15 @@ template <typename T> struct HalfRaw;
 template <> struct HalfRaw<bf16> { bf16x4 a, b; };
 template <> struct HalfRaw<float> { f32x4 a, b; };
 template <typename T, int DH>
-__device__ __forceinline__ HalfRaw<T> row8p(const T* t, int r, int c0, int lane) {
-  const int g = lane >> 4, c1 = DH >= 32 ? c0 + 16 : c0;
-  const T *p = t + Tile<T, DH>::off(r, c0 + 4 * g), *q = t + Tile<T, DH>::off(r, c1 + 4 * g);
-  if constexpr (sizeof(T) == 2) return {lds_read_b64(p), lds_read_b64(q)};
-  else return {lds_read_f32x4(p), lds_read_f32x4(q)};
+__device__ __forceinline__ unsigned half_base(const T* t, int r, int lane) {
+  return lds_addr(t + Tile<T, DH>::off(r, 4 * (lane >> 4)));
+}
+template <typename T, int DH, int KS, int R>
+__device__ __forceinline__ HalfRaw<T> half_at(unsigned a) {
+  constexpr int O = R * DH * (int)sizeof(T), C = 32 * KS * (int)sizeof(T);
+  constexpr int D = DH >= 32 ? 16 * (int)sizeof(T) : 0;
+  if constexpr (sizeof(T) == 2) return {lds_read_b64_at<O>(a ^ C), lds_read_b64_at<O>(a ^ (C + D))};
+  else return {lds_read_f32x4_at<O>(a ^ C), lds_read_f32x4_at<O>(a ^ (C + D))};
 }
 template <typename T, int DH>
 __device__ __forceinline__ typename Frag<T>::type take_row8p(HalfRaw<T>& r) {
@@ -93,22 +97,21 @@ __device__ __forceinline__ void add_outer(f32x4 (&S)[DH / 16], const T* At,
                                           const float (&w)[2][8], int lane) {
   typedef typename Frag<T>::type F;
   constexpr int NP = Parts<T>::N;
-#pragma unroll
-  for (int us = 0; us < 2; ++us) {
+  const ColBase<T> base = Tile<T, DH>::col_base(At, lane);
+  each<2>([&](auto us) __attribute__((always_inline)) {
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = w[us][e] == 0.f ? 0.f : w[us][e] * to_f32(cf[us][e]);
     F p[NP];
     split(x, p);
-#pragma unroll
-    for (int t = 0; t < DH / 16; ++t) {
-      ColRaw<T> ar = Tile<T, DH>::col8(At, us * 32, us * 32 + 16, t * 16, lane);
+    each<DH / 16>([&](auto t) __attribute__((always_inline)) {
+      ColRaw<T> ar = Tile<T, DH>::template col_at<t, us * 32, us * 32 + 16>(base, 0);
       lds_tr_wait();
       const F a = take(ar);
 #pragma unroll
       for (int n = NP - 1; n >= 0; --n) S[t] = mma16(a, p[n], S[t]);
-    }
-  }
+    });
+  });
 }
 
 // The wave's part of a [DH][DH] state in memory: rows 16t + 4g + r, column col.
@@ -166,7 +169,7 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
   constexpr int NI = TL::NCH / NW;  // loads of a tile by each wave
   __shared__ __attribute__((aligned(1024))) T lds[NB][3 - FIRST][kC * DH];
   __shared__ __attribute__((aligned(1024))) T P[STATE ? 16 : kC * kC];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int h = blockIdx.x % a.H;
   const LinSeg sg = lin_segment(a.cu, a.nseq, a.total, a.seg, blockIdx.x / a.H);
@@ -222,6 +225,12 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
   for (int ib = 0; ib < 4; ++ib) fi[ib] = a.s_inter * powg(lg2, ib * 16 + lr + EI);
   const float gC = powg(lg2, kC);
 
+  // this wave's columns of a tile: the column operand 16 wave .. + 15
+  auto own_cols = [&](ColRaw<T>(&r)[2], const T* t) __attribute__((always_inline)) {
+    ColBase<T> b = TL::col_base(t, lane);
+    for (auto& x : b.a) x ^= wave * 16 * (int)sizeof(T);
+    each<2>([&](auto us) { r[us] = TL::template col_at<0, us * 32, us * 32 + 16>(b, 0); });
+  };
   if (NB == 2 && nc > 0) {
     issue(0);
     vm_wait<0>();
@@ -252,17 +261,18 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
         const int jb = blk < 10 ? blk - ib * (ib + 1) / 2 : ib + 1;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
         if (blk < 10) {
+          const unsigned ra = TL::row_base(At, ib * 16 + lr, lane);
+          const unsigned rb = TL::row_base(Bt, jb * 16 + lr, lane);
           RowRaw<T> br[KS], ar[KS];
-#pragma unroll
-          for (int ds = 0; ds < KS; ++ds) {
-            br[ds] = TL::row8(Bt, jb * 16 + lr, ds * 32 + lg * 8);
-            ar[ds] = TL::row8(At, ib * 16 + lr, ds * 32 + lg * 8);
-          }
+          each<KS>([&](auto ds) {
+            br[ds] = TL::template row_at<ds, 0>(rb);
+            ar[ds] = TL::template row_at<ds, 0>(ra);
+          });
           lds_tr_wait();
 #pragma unroll
           for (int ds = 0; ds < KS; ++ds) {
-            const F bf = TL::take_row(br[ds], ds * 32 + lg * 8);
-            s = mma16(bf, TL::take_row(ar[ds], ds * 32 + lg * 8), s);
+            const F bf = TL::take_row(br[ds], lane);
+            s = mma16(bf, TL::take_row(ar[ds], lane), s);
           }
         }
         const int i = ib * 16 + lr;
@@ -276,24 +286,22 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
       // the state's term, while the scores arrive
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib) oa[ib] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
+      const unsigned ha = half_base<T, DH>(At, lr, lane);
+      each<KS>([&](auto ks) __attribute__((always_inline)) {
         const F sf = frag_from<T>(S[2 * ks], DH >= 32 ? S[2 * ks + (DH >= 32)] : f32x4{});
         HalfRaw<T> qr[4];
-#pragma unroll
-        for (int ib = 0; ib < 4; ++ib) qr[ib] = row8p<T, DH>(At, ib * 16 + lr, ks * 32, lane);
+        each<4>([&](auto ib) { qr[ib] = half_at<T, DH, ks, ib * 16>(ha); });
         lds_tr_wait();
 #pragma unroll
         for (int ib = 0; ib < 4; ++ib) oa[ib] = mma16(sf, take_row8p<T, DH>(qr[ib]), oa[ib]);
-      }
+      });
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib) oa[ib] *= fi[ib];
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the scores are written
       wg_barrier();
     }
     ColRaw<T> cr[2];
-#pragma unroll
-    for (int us = 0; us < 2; ++us) cr[us] = TL::col8(Ct, us * 32, us * 32 + 16, wave * 16, lane);
+    own_cols(cr, Ct);
     lds_tr_wait();
 #pragma unroll
     for (int us = 0; us < 2; ++us) cf[us] = take(cr[us]);
@@ -301,15 +309,15 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
       // A value that is not finite must not reach the rows before it through
       // 0 * inf: such columns are summed row by row.
       if (__ballot((nonfinite_bits(cf[0]) | nonfinite_bits(cf[1])) != 0) == 0) {
-#pragma unroll
-        for (int ib = 0; ib < 4; ++ib) {
-          RowRaw<T> pr[2];
-#pragma unroll
-          for (int us = 0; us <= ib / 2; ++us) pr[us] = TP::row8(P, ib * 16 + lr, us * 32 + lg * 8);
+        const unsigned pa = TP::row_base(P, lr, lane);
+        each<4>([&](auto ib) __attribute__((always_inline)) {
+          constexpr int NU = ib / 2 + 1;
+          RowRaw<T> pr[NU];
+          each<NU>([&](auto us) { pr[us] = TP::template row_at<us, ib * 16>(pa); });
           lds_tr_wait();
 #pragma unroll
-          for (int us = 0; us <= ib / 2; ++us) oa[ib] = mma16(cf[us], take(pr[us]), oa[ib]);
-        }
+          for (int us = 0; us < NU; ++us) oa[ib] = mma16(cf[us], take(pr[us]), oa[ib]);
+        });
       } else {
 #pragma unroll
         for (int ib = 0; ib < 4; ++ib) {
@@ -405,7 +413,7 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
   constexpr int NW = DH / 16, NT = DH / 16, KS = DH >= 32 ? DH / 32 : 1;
   constexpr int NI = TL::NCH / NW;
   __shared__ __attribute__((aligned(1024))) T lds[4][kC * DH];  // q, k, v, do
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int h = blockIdx.x % a.H, slot = blockIdx.x / a.H;
   const LinSeg sg = lin_segment(a.cu, a.nseq, a.total, a.seg, slot);
@@ -453,16 +461,16 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
     for (int blk = wave; blk < 10; blk += NW) {
       const int ib = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, jb = blk - ib * (ib + 1) / 2;
       f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ds = 0; ds < KS; ++ds) {
-        const int c0 = ds * 32 + lg * 8;
-        RowRaw<T> qr = TL::row8(lds[0], ib * 16 + lr, c0), kr = TL::row8(lds[1], jb * 16 + lr, c0);
-        RowRaw<T> vr = TL::row8(lds[2], jb * 16 + lr, c0), dr = TL::row8(lds[3], ib * 16 + lr, c0);
+      each<KS>([&](auto ds) __attribute__((always_inline)) {
+        RowRaw<T> qr = TL::template row_at<ds, 0>(TL::row_base(lds[0], ib * 16 + lr, lane));
+        RowRaw<T> kr = TL::template row_at<ds, 0>(TL::row_base(lds[1], jb * 16 + lr, lane));
+        RowRaw<T> vr = TL::template row_at<ds, 0>(TL::row_base(lds[2], jb * 16 + lr, lane));
+        RowRaw<T> dr = TL::template row_at<ds, 0>(TL::row_base(lds[3], ib * 16 + lr, lane));
         lds_tr_wait();
-        const F kf = TL::take_row(kr, c0), vf = TL::take_row(vr, c0);
-        s = mma16(kf, TL::take_row(qr, c0), s);
-        dp = mma16(vf, TL::take_row(dr, c0), dp);
-      }
+        const F kf = TL::take_row(kr, lane), vf = TL::take_row(vr, lane);
+        s = mma16(kf, TL::take_row(qr, lane), s);
+        dp = mma16(vf, TL::take_row(dr, lane), dp);
+      });
       const int i = ib * 16 + lr;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -472,11 +480,13 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
     }
     ColRaw<T> dr[2], vr[2];
     F df[2], vf[2];
-#pragma unroll
-    for (int us = 0; us < 2; ++us) {
-      dr[us] = TL::col8(lds[3], us * 32, us * 32 + 16, wave * 16, lane);
-      vr[us] = TL::col8(lds[2], us * 32, us * 32 + 16, wave * 16, lane);
-    }
+    ColBase<T> db = TL::col_base(lds[3], lane), vb = TL::col_base(lds[2], lane);
+    for (auto& x : db.a) x ^= wave * 16 * (int)sizeof(T);
+    for (auto& x : vb.a) x ^= wave * 16 * (int)sizeof(T);
+    each<2>([&](auto us) {
+      dr[us] = TL::template col_at<0, us * 32, us * 32 + 16>(db, 0);
+      vr[us] = TL::template col_at<0, us * 32, us * 32 + 16>(vb, 0);
+    });
     lds_tr_wait();
 #pragma unroll
     for (int us = 0; us < 2; ++us) {

@@ -14,6 +14,8 @@
 // next row bit goes to the highest chunk bit.
 #pragma once
 
+#include <utility>
+
 #include "common.h"
 
 namespace bcmt {
@@ -49,6 +51,25 @@ __device__ __forceinline__ f32x8 take(ColRaw<float>& r) {
   return f32x8{r.e[0], r.e[1], r.e[2], r.e[3], r.e[4], r.e[5], r.e[6], r.e[7]};
 }
 
+// The addresses of a lane's column operands: one with the transposing reads,
+// one for each of four rows otherwise.
+template <typename T> struct ColBase { unsigned a[sizeof(T) == 2 ? 1 : 4]; };
+
+template <class P>
+__device__ __forceinline__ unsigned lds_addr(const P* p) {
+  return (unsigned)(uintptr_t)((__attribute__((address_space(3))) P*)(p));
+}
+
+// f(0), ..., f(N - 1) with the index as a constant.
+template <class Fn, int... I>
+__device__ __forceinline__ void each_(Fn& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class Fn>
+__device__ __forceinline__ void each(Fn f) {
+  each_(f, std::make_integer_sequence<int, N>{});
+}
+
 template <typename T, int DH>
 struct Tile {
   static constexpr int CH = 16 / (int)sizeof(T);  // elements of a chunk
@@ -73,38 +94,64 @@ struct Tile {
     __builtin_amdgcn_global_load_lds(src + (int64_t)grow * ld + ((pos ^ swz(row)) * CH),
                                      (lds_void_t*)(t + i * 64 * CH), 16, 0, 0);
   }
-  // Row operand: elements c0 .. c0 + 7 of row r, zero from column DH on (rows
-  // narrower than a product's 32 columns).
-  __device__ static __forceinline__ RowRaw<T> row8(const T* t, int r, int c0) {
-    const int c = DH >= 32 || c0 < DH ? c0 : 0;
-    if constexpr (sizeof(T) == 2) return {lds_read_b128(t + off(r, c))};
-    else return {lds_read_f32x4(t + off(r, c)), lds_read_f32x4(t + off(r, c + 4))};
+  // The reads of a tile go by a byte address of the lane, formed once, an
+  // exclusive or for the columns (a row begins at a multiple of its size, so
+  // that the or only permutes its chunks) and a constant offset for the rows.
+  //
+  // Row operand: elements 32 DS + 8g .. + 7, g = lane / 16, of row r + R; zero
+  // where a row is narrower than a product's 32 columns.
+  __device__ static __forceinline__ unsigned row_base(const T* t, int r, int lane) {
+    const int c = (lane >> 4) * 8;
+    return lds_addr(t + off(r, DH >= 32 || c < DH ? c : 0));
   }
-  __device__ static __forceinline__ typename Frag<T>::type take_row(RowRaw<T>& r, int c0) {
+  template <int DS, int R>
+  __device__ static __forceinline__ RowRaw<T> row_at(unsigned a) {
+    constexpr int O = R * DH * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2) return {lds_read_b128_at<O>(a ^ (DS * 64))};
+    else return {lds_read_f32x4_at<O>(a ^ (DS * 128)), lds_read_f32x4_at<O>(a ^ (DS * 128 + 16))};
+  }
+  __device__ static __forceinline__ typename Frag<T>::type take_row(RowRaw<T>& r, int lane) {
     typedef typename Frag<T>::type F;
     const F f = take(r);
-    return DH >= 32 || c0 < DH ? f : F{};
+    return DH >= 32 || (lane >> 4) * 8 < DH ? f : F{};
   }
-  // Column operand: column c0 + lane % 16 of rows b0 + 4g .. + 3 and
-  // b1 + 4g .. + 3, g = lane / 16: the order in which two 16-row result tiles
-  // hold their rows.
-  __device__ static __forceinline__ ColRaw<T> col8(const T* t, int b0, int b1, int c0, int lane) {
+  // Column operand: column 16 JJ + lane % 16 of rows B0 + 4g .. + 3 and
+  // B1 + 4g .. + 3: the order in which two 16-row result tiles hold their rows.
+  __device__ static __forceinline__ ColBase<T> col_base(const T* t, int lane) {
     const int g = lane >> 4, i = lane & 15;
     if constexpr (sizeof(T) == 2) {
-      const int rr = 4 * g + (i >> 2), cc = c0 + ((i & 3) << 2);
-      return {lds_read_tr(t + off(b0 + rr, cc)), lds_read_tr(t + off(b1 + rr, cc))};
+      return {{lds_addr(t + off(4 * g + (i >> 2), (i & 3) << 2))}};
+    } else {
+      ColBase<T> r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.a[e] = lds_addr(t + off(4 * g + e, i));
+      return r;
+    }
+  }
+  template <int JJ, int B0, int B1>
+  __device__ static __forceinline__ ColRaw<T> col_at(const ColBase<T>& b, unsigned add) {
+    constexpr int O0 = B0 * DH * (int)sizeof(T), O1 = B1 * DH * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2) {
+      const unsigned a = (b.a[0] ^ (JJ * 32)) + add;
+      return {lds_read_tr_at<O0>(a), lds_read_tr_at<O1>(a)};
     } else {
       ColRaw<T> r;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        r.e[e] = lds_read_f32(t + off(b0 + 4 * g + e, c0 + i));
-        r.e[4 + e] = lds_read_f32(t + off(b1 + 4 * g + e, c0 + i));
-      }
+      each<4>([&](auto e) {
+        const unsigned a = (b.a[e] ^ (JJ * 64)) + add;
+        r.e[e] = lds_read_f32_at<O0>(a);
+        r.e[4 + e] = lds_read_f32_at<O1>(a);
+      });
       return r;
     }
   }
 };
 
+// The wave's index as a scalar.  Branches on it must be scalar branches: a
+// matrix instruction ignores the lane mask, so in a block that is skipped by
+// masking every lane off it would still write its result.
+__device__ __forceinline__ int wave_index() {
+  return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+}
 // Workgroup barrier without the vmcnt drain of __syncthreads(): direct loads
 // stay in flight, and no memory access moves across it.
 __device__ __forceinline__ void wg_barrier() {

@@ -17,6 +17,9 @@
 // the second operand of the next product as they are (Tile::col8 reads the
 // first operand in the same key order).  dK/dV computes them untransposed,
 // one key per lane, to the same end.
+#include <climits>
+#include <type_traits>
+
 #include "kernels.h"
 #include "mixer_tile.h"
 
@@ -51,9 +54,17 @@ __device__ __forceinline__ void issue_pair(const T* a, int64_t lda, const T* b, 
 // ------------------------------------------------------------------ forward
 // One workgroup of four waves: 64 NQ queries of one head, NQ groups of 16 per
 // wave.  Tiles of 64 keys, double buffered; running maximum and sum.
+//
+// The maximum is raised only when a score passes it by more than 2^kRaise: the
+// weights then stay below 2^kRaise (their relative rounding is the same at any
+// scale, and float32 sums have the room), and the outputs are rescaled, and the
+// lanes of a row agree on its maximum, in a few tiles of a sequence instead of
+// in all.  Tiles that every query of a wave sees whole take no mask.
+
+constexpr float kRaise = 8.f;
 
 template <typename T, int DH, int NQ>
-__global__ __launch_bounds__(256) void seq_fwd_kernel(
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_fwd_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const int* __restrict__ cu, T* __restrict__ o, float* __restrict__ lse, int total, int nseq,
     int H, int G, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2) {
@@ -61,9 +72,9 @@ __global__ __launch_bounds__(256) void seq_fwd_kernel(
   typedef Tile<T, DH> TL;
   constexpr int NW = 4, QT = NW * 16 * NQ, KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
   constexpr int NI = 2 * TL::NCH / NW;
-  constexpr int KUS = sizeof(T) == 2 ? 4 : 1;  // key groups whose fragments are live at once
+  constexpr int KUS = sizeof(T) == 2 ? (DH > 64 ? 2 : 4) : 1;  // key groups read at once
   __shared__ __attribute__((aligned(1024))) T lds[2][2][64 * DH];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int nslot = total / QT + nseq;
   const int h = blockIdx.x % H;
@@ -99,6 +110,112 @@ __global__ __launch_bounds__(256) void seq_fwd_kernel(
     for (int jj = 0; jj < NJ; ++jj) oa[nq][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  int dropped = INT_MAX;  // first tile of which a value was left out
+  constexpr unsigned BUF = 2 * 64 * DH * sizeof(T);
+  const unsigned krow = TL::row_base(lds[0][0], lr, lane);
+  const ColBase<T> vcol = TL::col_base(lds[0][1], lane);
+  auto tile = [&](auto masked, int kt, int buf) __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(masked)::value;
+    const unsigned ba = buf * BUF, ka = krow + ba;
+    bool live[NQ];
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq)
+      live[nq] = !MASK || !(tq[nq] >= be || tq[nq] + 15 < kt);  // wave-uniform
+    f32x4 s[NQ][4];
+    each<4 / KUS>([&](auto kk) __attribute__((always_inline)) {
+      constexpr int k0 = kk * KUS;
+      RowRaw<T> kr[KUS][KS];
+      each<KUS>([&](auto ku) {
+        each<KS>([&](auto ds) { kr[ku][ds] = TL::template row_at<ds, (k0 + ku) * 16>(ka); });
+      });
+      lds_tr_wait();
+#pragma unroll
+      for (int ku = 0; ku < KUS; ++ku) {
+        F kf[KS];
+#pragma unroll
+        for (int ds = 0; ds < KS; ++ds) kf[ds] = TL::take_row(kr[ku][ds], lane);
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+          s[nq][k0 + ku] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds)
+            s[nq][k0 + ku] = mma16(kf[ds], qf[nq][ds], s[nq][k0 + ku]);
+        }
+      }
+    });
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+      if (MASK) {
+        const int t_eff = live[nq] ? min(tq[nq] + lr, be - 1) : -1;
+#pragma unroll
+        for (int ku = 0; ku < 4; ++ku)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (kt + ku * 16 + lg * 4 + r > t_eff) s[nq][ku][r] = -INFINITY;
+      }
+      float mx = s[nq][0][0];
+#pragma unroll
+      for (int ku = 0; ku < 4; ++ku)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[nq][ku][r]);
+      mx *= sl2;
+      if (__ballot(mx > m[nq] + kRaise) != 0) {  // (m = -inf: any finite score)
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float mnew = fmaxf(m[nq], mx);
+        const float alpha = exp2_fast(m[nq] - (mnew == -INFINITY ? 0.f : mnew));
+        l[nq] *= alpha;
+        m[nq] = mnew;
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) oa[nq][jj] *= alpha;
+      }
+      // all scores so far -inf: subtract 0, so that the weights are 0 and later
+      // finite scores still count
+      const float neg = m[nq] == -INFINITY ? 0.f : -m[nq];
+      float ps = 0.f;
+#pragma unroll
+      for (int ku = 0; ku < 4; ++ku)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = exp2_fast(fmaf(s[nq][ku][r], sl2, neg));
+          s[nq][ku][r] = p;
+          ps += p;
+        }
+      l[nq] += ps;
+    }
+    each<2>([&](auto us) __attribute__((always_inline)) {
+      ColRaw<T> vr[NJ];
+      each<NJ>([&](auto jj) { vr[jj] = TL::template col_at<jj, us * 32, us * 32 + 16>(vcol, ba); });
+      lds_tr_wait();
+      F vf[NJ];
+#pragma unroll
+      for (int jj = 0; jj < NJ; ++jj) vf[jj] = take(vr[jj]);
+      // 0 * inf would reach the queries that do not see an infinite or NaN value:
+      // such values count as 0 here and are added at the end, to the rows that
+      // see them.
+      if (MASK) {
+        unsigned bad = 0;
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) bad |= nonfinite_bits(vf[jj]);
+        if (__ballot(bad != 0) != 0) {
+          dropped = min(dropped, kt);
+#pragma unroll
+          for (int jj = 0; jj < NJ; ++jj)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (!(fabsf(to_f32(vf[jj][e])) < INFINITY)) vf[jj][e] = from_f32<T>(0.f);
+        }
+      }
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        if (!live[nq]) continue;
+        const F pf = frag_from<T>(s[nq][2 * us], s[nq][2 * us + 1]);
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) oa[nq][jj] = mma16(vf[jj], pf, oa[nq][jj]);
+      }
+    });
+  };
+
   issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs, kend - 1, lds[0][0], lds[0][1], wave, lane);
   if (nt > 1)
     issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + 64, kend - 1, lds[1][0], lds[1][1], wave, lane);
@@ -107,123 +224,8 @@ __global__ __launch_bounds__(256) void seq_fwd_kernel(
     else vm_wait<0>();
     wg_barrier();
     const int kt = bs + it * 64;
-    const T* Kt = lds[it & 1][0];
-    const T* Vt = lds[it & 1][1];
-    bool live[NQ], any = false;
-#pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) {
-      live[nq] = !(tq[nq] >= be || tq[nq] + 15 < kt);  // wave-uniform
-      any |= live[nq];
-    }
-    if (any) {
-      f32x4 s[NQ][4];
-#pragma unroll
-      for (int k0 = 0; k0 < 4; k0 += KUS) {
-        RowRaw<T> kr[KUS][KS];
-#pragma unroll
-        for (int ku = 0; ku < KUS; ++ku)
-#pragma unroll
-          for (int ds = 0; ds < KS; ++ds)
-            kr[ku][ds] = TL::row8(Kt, (k0 + ku) * 16 + lr, ds * 32 + lg * 8);
-        lds_tr_wait();
-#pragma unroll
-        for (int ku = 0; ku < KUS; ++ku) {
-          F kf[KS];
-#pragma unroll
-          for (int ds = 0; ds < KS; ++ds) kf[ds] = TL::take_row(kr[ku][ds], ds * 32 + lg * 8);
-#pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) {
-            s[nq][k0 + ku] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ds = 0; ds < KS; ++ds)
-              s[nq][k0 + ku] = mma16(kf[ds], qf[nq][ds], s[nq][k0 + ku]);
-          }
-        }
-      }
-#pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) {
-        if (!live[nq]) continue;
-        const int t_eff = min(tq[nq] + lr, be - 1);
-        float mx = -INFINITY;
-#pragma unroll
-        for (int ku = 0; ku < 4; ++ku)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int u = kt + ku * 16 + lg * 4 + r;
-            const float z = u <= t_eff ? s[nq][ku][r] * sl2 : -INFINITY;
-            s[nq][ku][r] = z;
-            mx = fmaxf(mx, z);
-          }
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float mnew = fmaxf(m[nq], mx);
-        // all scores so far -inf: subtract 0, so that the weights are 0 and
-        // later finite scores still count
-        const float ms = mnew == -INFINITY ? 0.f : mnew;
-        const float alpha = exp2_fast(m[nq] - ms);
-        float ps = 0.f;
-#pragma unroll
-        for (int ku = 0; ku < 4; ++ku)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = exp2_fast(s[nq][ku][r] - ms);
-            s[nq][ku][r] = p;
-            ps += p;
-          }
-        l[nq] = l[nq] * alpha + ps;
-        m[nq] = mnew;
-#pragma unroll
-        for (int jj = 0; jj < NJ; ++jj) oa[nq][jj] *= alpha;
-      }
-      // A value that is not finite, in a row that some query of the tile does
-      // not see: 0 * inf would reach that query through the products.  Such a
-      // half tile is summed key by key over the visible rows instead.
-#pragma unroll
-      for (int us = 0; us < 2; ++us) {
-        ColRaw<T> vr[NJ];
-#pragma unroll
-        for (int jj = 0; jj < NJ; ++jj) vr[jj] = TL::col8(Vt, us * 32, us * 32 + 16, jj * 16, lane);
-        lds_tr_wait();
-        F vf[NJ];
-#pragma unroll
-        for (int jj = 0; jj < NJ; ++jj) vf[jj] = take(vr[jj]);
-        bool slow = false;
-        if (kt + us * 32 + 31 > q0) {
-          unsigned bad = 0;
-#pragma unroll
-          for (int jj = 0; jj < NJ; ++jj) bad |= nonfinite_bits(vf[jj]);
-          slow = __ballot(bad != 0) != 0;
-        }
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) {
-          if (!live[nq]) continue;
-          if (!slow) {
-            const F pf = frag_from<T>(s[nq][2 * us], s[nq][2 * us + 1]);
-#pragma unroll
-            for (int jj = 0; jj < NJ; ++jj) oa[nq][jj] = mma16(vf[jj], pf, oa[nq][jj]);
-            continue;
-          }
-          const int t_eff = min(tq[nq] + lr, be - 1);
-#pragma unroll 1
-          for (int gg = 0; gg < 4; ++gg)
-#pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const int ui = us * 32 + k2 * 16 + gg * 4 + r;
-                const float p =
-                    to_f32(from_f32<T>(__shfl(s[nq][2 * us + k2][r], lr + 16 * gg, 64)));
-                if (kt + ui > t_eff) continue;
-#pragma unroll
-                for (int jj = 0; jj < NJ; ++jj) {
-                  const f32x4 vv = load4f(Vt + TL::off(ui, jj * 16 + lg * 4));
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) oa[nq][jj][e] = fmaf(p, vv[e], oa[nq][jj][e]);
-                }
-              }
-        }
-      }
-    }
+    if (kt + 63 <= tq[0]) tile(std::false_type{}, kt, it & 1);
+    else if (kt <= min(tq[NQ - 1] + 15, be - 1)) tile(std::true_type{}, kt, it & 1);
     if (it + 2 < nt) {
       wg_barrier();  // every wave is done with this buffer
       issue_pair<T, DH, NW>(kb, ldk, vb, ldv, kt + 128, kend - 1, lds[it & 1][0], lds[it & 1][1],
@@ -231,6 +233,16 @@ __global__ __launch_bounds__(256) void seq_fwd_kernel(
     }
   }
 
+  for (int u = dropped; u < min(be, tq[NQ - 1] + 16); ++u)  // (none, as a rule)
+#pragma unroll
+    for (int jj = 0; jj < NJ; ++jj) {
+      const f32x4 x = load4f(vb + (int64_t)u * ldv + jj * 16 + lg * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq)
+          if (u <= tq[nq] + lr && !(fabsf(x[e]) < INFINITY)) oa[nq][jj][e] += x[e];
+    }
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
     float lt = l[nq];
@@ -264,7 +276,7 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
   constexpr int NW = 4, QT = NW * 16 * NQ, KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
   constexpr int NI = 2 * TL::NCH / NW;
   __shared__ __attribute__((aligned(1024))) T lds[2][2][64 * DH];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int nslot = total / QT + nseq;
   const int h = blockIdx.x % H;
@@ -307,6 +319,9 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
   for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
     for (int jj = 0; jj < NJ; ++jj) da[nq][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+  constexpr unsigned BUF = 2 * 64 * DH * sizeof(T);
+  const unsigned krow = TL::row_base(lds[0][0], lr, lane), vrow = TL::row_base(lds[0][1], lr, lane);
+  const ColBase<T> kcol = TL::col_base(lds[0][0], lane);
 
   issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs, kend - 1, lds[0][0], lds[0][1], wave, lane);
   if (nt > 1)
@@ -316,8 +331,7 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
     else vm_wait<0>();
     wg_barrier();
     const int kt = bs + it * 64;
-    const T* Kt = lds[it & 1][0];
-    const T* Vt = lds[it & 1][1];
+    const unsigned ba = (it & 1) * BUF;
     bool live[NQ], any = false;
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
@@ -326,24 +340,21 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
     }
     if (any) {
       // 32 keys at a time: scores and dp of two key groups, then their part of dQ
-#pragma unroll
-      for (int us = 0; us < 2; ++us) {
+      each<2>([&](auto us) __attribute__((always_inline)) {
         f32x4 s[NQ][2];
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2) {
-          const int ku = us * 2 + k2;
+        each<2>([&](auto k2) __attribute__((always_inline)) {
+          constexpr int ku = us * 2 + k2;
           RowRaw<T> kr[KS], vr[KS];
-#pragma unroll
-          for (int ds = 0; ds < KS; ++ds) {
-            kr[ds] = TL::row8(Kt, ku * 16 + lr, ds * 32 + lg * 8);
-            vr[ds] = TL::row8(Vt, ku * 16 + lr, ds * 32 + lg * 8);
-          }
+          each<KS>([&](auto ds) {
+            kr[ds] = TL::template row_at<ds, ku * 16>(krow + ba);
+            vr[ds] = TL::template row_at<ds, ku * 16>(vrow + ba);
+          });
           lds_tr_wait();
           F kf[KS], vf[KS];
 #pragma unroll
           for (int ds = 0; ds < KS; ++ds) {
-            kf[ds] = TL::take_row(kr[ds], ds * 32 + lg * 8);
-            vf[ds] = TL::take_row(vr[ds], ds * 32 + lg * 8);
+            kf[ds] = TL::take_row(kr[ds], lane);
+            vf[ds] = TL::take_row(vr[ds], lane);
           }
 #pragma unroll
           for (int nq = 0; nq < NQ; ++nq) {
@@ -361,20 +372,19 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
                   u <= t_eff ? exp2_fast(sv[r] * sl2 - ls[nq]) * (dp[r] - dl[nq]) : 0.f;
             }
           }
-        }
+        });
         F zf[NQ];
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) zf[nq] = frag_from<T>(s[nq][0], s[nq][1]);
-#pragma unroll
-        for (int jj = 0; jj < NJ; ++jj) {
-          ColRaw<T> kr = TL::col8(Kt, us * 32, us * 32 + 16, jj * 16, lane);
+        each<NJ>([&](auto jj) __attribute__((always_inline)) {
+          ColRaw<T> kr = TL::template col_at<jj, us * 32, us * 32 + 16>(kcol, ba);
           lds_tr_wait();
           const F kc = take(kr);
 #pragma unroll
           for (int nq = 0; nq < NQ; ++nq)
             if (live[nq]) da[nq][jj] = mma16(kc, zf[nq], da[nq][jj]);
-        }
-      }
+        });
+      });
     }
     if (it + 2 < nt) {
       wg_barrier();
@@ -413,7 +423,7 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
   constexpr int NI = 2 * TL::NCH / NW + 1;
   __shared__ __attribute__((aligned(1024))) T lds[2][2][64 * DH];
   __shared__ __attribute__((aligned(16))) float rows[2][NW][64];  // lse, delta: waves 0 and 1
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int Hkv = H / G;
   const int j = blockIdx.x % Hkv;
@@ -449,6 +459,9 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
     __builtin_amdgcn_global_load_lds(src, (lds_void_t*)rows[it & 1][wave], 4, 0, 0);
   };
 
+  constexpr unsigned BUF = 2 * 64 * DH * sizeof(T);
+  const unsigned qrow = TL::row_base(lds[0][0], lr, lane), drow = TL::row_base(lds[0][1], lr, lane);
+  const ColBase<T> qcol = TL::col_base(lds[0][0], lane), dcol = TL::col_base(lds[0][1], lane);
   issue(0);
   if (nt > 1) issue(1);
   for (int it = 0; it < nt; ++it) {
@@ -456,8 +469,7 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
     else vm_wait<0>();
     wg_barrier();
     const int tt = k0 + (it % nt1) * 64;
-    const T* Qt = lds[it & 1][0];
-    const T* Dt = lds[it & 1][1];
+    const unsigned ba = (it & 1) * BUF;
     bool live[NK], any = false;
 #pragma unroll
     for (int nk = 0; nk < NK; ++nk) {
@@ -466,26 +478,23 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
     }
     if (any) {
       // 32 queries at a time
-#pragma unroll
-      for (int us = 0; us < 2; ++us) {
+      each<2>([&](auto us) __attribute__((always_inline)) {
         f32x4 p[NK][2], z[NK][2];
-#pragma unroll
-        for (int t2 = 0; t2 < 2; ++t2) {
-          const int ts = us * 2 + t2;
+        each<2>([&](auto t2) __attribute__((always_inline)) {
+          constexpr int ts = us * 2 + t2;
           RowRaw<T> qr[KS], dr[KS];
-#pragma unroll
-          for (int ds = 0; ds < KS; ++ds) {
-            qr[ds] = TL::row8(Qt, ts * 16 + lr, ds * 32 + lg * 8);
-            dr[ds] = TL::row8(Dt, ts * 16 + lr, ds * 32 + lg * 8);
-          }
+          each<KS>([&](auto ds) {
+            qr[ds] = TL::template row_at<ds, ts * 16>(qrow + ba);
+            dr[ds] = TL::template row_at<ds, ts * 16>(drow + ba);
+          });
           f32x4 ls = lds_read_f32x4(&rows[it & 1][0][ts * 16 + lg * 4]);
           f32x4 dl = lds_read_f32x4(&rows[it & 1][1][ts * 16 + lg * 4]);
           lds_tr_wait();
           F qf[KS], df[KS];
 #pragma unroll
           for (int ds = 0; ds < KS; ++ds) {
-            qf[ds] = TL::take_row(qr[ds], ds * 32 + lg * 8);
-            df[ds] = TL::take_row(dr[ds], ds * 32 + lg * 8);
+            qf[ds] = TL::take_row(qr[ds], lane);
+            df[ds] = TL::take_row(dr[ds], lane);
           }
           lds_tr_bind(ls);
           lds_tr_bind(dl);
@@ -507,17 +516,16 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
               z[nk][t2][r] = ok ? pv * (dp[r] - dl[r]) : 0.f;
             }
           }
-        }
+        });
         F pf[NK], zf[NK];
 #pragma unroll
         for (int nk = 0; nk < NK; ++nk) {
           pf[nk] = frag_from<T>(p[nk][0], p[nk][1]);
           zf[nk] = frag_from<T>(z[nk][0], z[nk][1]);
         }
-#pragma unroll
-        for (int jj = 0; jj < NJ; ++jj) {
-          ColRaw<T> dr = TL::col8(Dt, us * 32, us * 32 + 16, jj * 16, lane);
-          ColRaw<T> qr = TL::col8(Qt, us * 32, us * 32 + 16, jj * 16, lane);
+        each<NJ>([&](auto jj) __attribute__((always_inline)) {
+          ColRaw<T> dr = TL::template col_at<jj, us * 32, us * 32 + 16>(dcol, ba);
+          ColRaw<T> qr = TL::template col_at<jj, us * 32, us * 32 + 16>(qcol, ba);
           lds_tr_wait();
           const F dc = take(dr), qc = take(qr);
 #pragma unroll
@@ -526,8 +534,8 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
               va[nk][jj] = mma16(dc, pf[nk], va[nk][jj]);
               ka[nk][jj] = mma16(qc, zf[nk], ka[nk][jj]);
             }
-        }
-      }
+        });
+      });
     }
     if (it + 2 < nt) {
       wg_barrier();
@@ -605,7 +613,7 @@ __global__ __launch_bounds__((DecShape<T, DH>::NW * 64)) void dec_part_kernel(De
   static_assert(NI >= 1 && NI * 64 == KT * TL::NCH, "tile loads");
   __shared__ __attribute__((aligned(1024))) T lds[NW][2][2][KT * DH];
   __shared__ float red_m[NW][16], red_l[NW][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int G = a.H / a.Hkv, NH = (G + 15) / 16;
   const int part = blockIdx.x, y = blockIdx.y;
@@ -645,6 +653,8 @@ __global__ __launch_bounds__((DecShape<T, DH>::NW * 64)) void dec_part_kernel(De
 #pragma unroll
     for (int i = 0; i < NI; ++i) TL::issue(vc, a.ct, t * KT, n, lds[wave][buf][1], i, lane);
   };
+  const unsigned krow = TL::row_base(lds[wave][0][0], lr, lane);
+  const ColBase<T> vcol = TL::col_base(lds[wave][0][1], lane);
   int t = t0 + wave, buf = 0;
   if (t < t1) issue(t, 0);
   if (t + NW < t1) issue(t + NW, 1);
@@ -672,20 +682,17 @@ __global__ __launch_bounds__((DecShape<T, DH>::NW * 64)) void dec_part_kernel(De
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     f32x4 s[2];
+    const unsigned ba = buf * 2 * KT * DH * sizeof(T);
     ColRaw<T> vr[NJ];
-#pragma unroll
-    for (int ku = 0; ku < 2; ++ku) {
+    each<2>([&](auto ku) {
       RowRaw<T> kr[KS];
-#pragma unroll
-      for (int ds = 0; ds < KS; ++ds) kr[ds] = TL::row8(Kt, ku * 16 + lr, ds * 32 + lg * 8);
+      each<KS>([&](auto ds) { kr[ds] = TL::template row_at<ds, ku * 16>(krow + ba); });
       lds_tr_wait();
       s[ku] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ds = 0; ds < KS; ++ds)
-        s[ku] = mma16(TL::take_row(kr[ds], ds * 32 + lg * 8), qf[ds], s[ku]);
-    }
-#pragma unroll
-    for (int jj = 0; jj < NJ; ++jj) vr[jj] = TL::col8(Vt, 0, 16, jj * 16, lane);
+      for (int ds = 0; ds < KS; ++ds) s[ku] = mma16(TL::take_row(kr[ds], lane), qf[ds], s[ku]);
+    });
+    each<NJ>([&](auto jj) { vr[jj] = TL::template col_at<jj, 0, 16>(vcol, ba); });
     float mx = -INFINITY;
 #pragma unroll
     for (int ku = 0; ku < 2; ++ku)
