@@ -231,10 +231,10 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
     for (auto& x : b.a) x ^= wave * 16 * (int)sizeof(T);
     each<2>([&](auto us) { r[us] = TL::template col_at<0, us * 32, us * 32 + 16>(b, 0); });
   };
-  if (NB == 2 && nc > 0) {
-    issue(0);
-    vm_wait<0>();
-  }
+  if (NB == 2 && nc > 0) issue(0);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) settle(S[t]);
+  if (NB == 2) vm_wait<0>();
   for (int c = 0; c < nc; ++c) {
     wg_barrier();  // this chunk's tiles are there; every wave is done with the last chunk
     if (NB == 2) {

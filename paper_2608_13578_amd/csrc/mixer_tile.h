@@ -152,6 +152,14 @@ struct Tile {
 __device__ __forceinline__ int wave_index() {
   return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 }
+// Waits here for a value loaded from global memory.  The compiler does not see
+// the waits of vm_wait(): a value still in flight where a loop begins would be
+// waited for inside the loop, together with every tile requested since.
+template <class V>
+__device__ __forceinline__ void settle(V& v) {
+  asm volatile("" : "+v"(v));
+}
+
 // Workgroup barrier without the vmcnt drain of __syncthreads(): direct loads
 // stay in flight, and no memory access moves across it.
 __device__ __forceinline__ void wg_barrier() {

@@ -36,24 +36,31 @@ __device__ __forceinline__ typename Frag<T>::type gfrag(const T* p, bool ok) {
 }
 
 // The two tiles (K, V or Q, dO) of one step, 2 NCH wave instructions shared by
-// NW waves.
+// NW waves (the first 2 NCH of them where there are more waves).
+template <typename T, int DH, int NW>
+constexpr int kPairLoads = 2 * Tile<T, DH>::NCH / NW > 1 ? 2 * Tile<T, DH>::NCH / NW : 1;
 template <typename T, int DH, int NW>
 __device__ __forceinline__ void issue_pair(const T* a, int64_t lda, const T* b, int64_t ldb, int r0,
                                            int rlast, T* ta, T* tb, int wave, int lane) {
   typedef Tile<T, DH> TL;
-  constexpr int NI = 2 * TL::NCH / NW;
-  static_assert(NI >= 1 && NI * NW == 2 * TL::NCH, "loads of two tiles");
+  constexpr int NI = kPairLoads<T, DH, NW>;
+  static_assert(NI * NW == 2 * TL::NCH || NI == 1, "loads of two tiles");
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int gi = wave * NI + i;
     if (gi < TL::NCH) TL::issue(a, lda, r0, rlast, ta, gi, lane);
-    else TL::issue(b, ldb, r0, rlast, tb, gi - TL::NCH, lane);
+    else if (gi < 2 * TL::NCH) TL::issue(b, ldb, r0, rlast, tb, gi - TL::NCH, lane);
   }
 }
 
 // ------------------------------------------------------------------ forward
-// One workgroup of four waves: 64 NQ queries of one head, NQ groups of 16 per
-// wave.  Tiles of 64 keys, double buffered; running maximum and sum.
+// One workgroup of NW waves, NQ groups of 16 queries each, over NW / wph heads of
+// one group (wph waves a head): every tile of 64 keys is fetched once for all of
+// them.  The tiles go through a ring of NS buffers, one barrier a tile.  Four
+// waves over 128 queries, two workgroups per CU and double buffers left a CU
+// waiting for its keys more than half of the time (16384 rows, 16 heads of 128:
+// 866 us, 471 us with the loads left out); eight waves halve the traffic, and
+// three tiles ahead hide the rest.
 //
 // The maximum is raised only when a score passes it by more than 2^kRaise: the
 // weights then stay below 2^kRaise (their relative rounding is the same at any
@@ -63,32 +70,39 @@ __device__ __forceinline__ void issue_pair(const T* a, int64_t lda, const T* b, 
 
 constexpr float kRaise = 8.f;
 
-template <typename T, int DH, int NQ>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_fwd_kernel(
+template <typename T, int DH> struct FwdShape {
+  static constexpr int NW = sizeof(T) == 2 ? 8 : 4, NQ = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int NS = sizeof(T) == 2 ? 4 : DH == 128 ? 2 : 3;
+};
+
+template <typename T, int DH>
+__global__ __launch_bounds__((FwdShape<T, DH>::NW * 64)) void seq_fwd_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const int* __restrict__ cu, T* __restrict__ o, float* __restrict__ lse, int total, int nseq,
-    int H, int G, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2) {
+    int H, int G, int wph, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
-  constexpr int NW = 4, QT = NW * 16 * NQ, KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
-  constexpr int NI = 2 * TL::NCH / NW;
+  constexpr int NW = FwdShape<T, DH>::NW, NQ = FwdShape<T, DH>::NQ, NS = FwdShape<T, DH>::NS;
+  constexpr int KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
+  constexpr int NI = kPairLoads<T, DH, NW>;
   constexpr int KUS = sizeof(T) == 2 ? (DH > 64 ? 2 : 4) : 1;  // key groups read at once
-  __shared__ __attribute__((aligned(1024))) T lds[2][2][64 * DH];
+  __shared__ __attribute__((aligned(1024))) T lds[NS][2][64 * DH];
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
-  const int nslot = total / QT + nseq;
-  const int h = blockIdx.x % H;
-  const SeqTile st = find_tile(cu, nseq, total, QT, nslot - 1 - (int)(blockIdx.x / H));
+  const int QT = wph * 16 * NQ, hp = NW / wph, HG = H / hp;
+  const int nslot = total / QT + nseq, wq = wave % wph;
+  const int h = (int)(blockIdx.x % HG) * hp + wave / wph;
+  const SeqTile st = find_tile(cu, nseq, total, QT, nslot - 1 - (int)(blockIdx.x / HG));
   const int bs = st.begin, be = st.end, q0 = bs + st.tile * QT;
   if (st.tile < 0 || q0 >= be) return;
   const int j = h / G;
   const T* kb = k + j * DH;
   const T* vb = v + j * DH;
-  // Groups of 16 queries are dealt w, 2 NW - 1 - w: a causal group's work grows
-  // with its position.
+  // A head's groups of 16 queries are dealt w, 2 wph - 1 - w: a causal group's work
+  // grows with its position.
   int tq[NQ];
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) tq[nq] = q0 + 16 * (nq & 1 ? 2 * NW - 1 - wave : wave);
+  for (int nq = 0; nq < NQ; ++nq) tq[nq] = q0 + 16 * (nq & 1 ? 2 * wph - 1 - wq : wq);
   const int kend = min(be, q0 + QT);
   const int nt = (kend - bs + 63) / 64;
 
@@ -216,21 +230,28 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_fwd_kernel(
     });
   };
 
-  issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs, kend - 1, lds[0][0], lds[0][1], wave, lane);
-  if (nt > 1)
-    issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + 64, kend - 1, lds[1][0], lds[1][1], wave, lane);
+  auto issue = [&](int it, int buf) __attribute__((always_inline)) {
+    issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + it * 64, kend - 1, lds[buf][0], lds[buf][1], wave,
+                          lane);
+  };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (i < nt) issue(i, i);
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) settle(qf[nq][ds]);
+  int buf = 0, next = NS - 1;
   for (int it = 0; it < nt; ++it) {
-    if (it + 1 < nt) vm_wait<NI>();
+    if (it + NS - 2 < nt) vm_wait<(NS - 2) * NI>();
     else vm_wait<0>();
-    wg_barrier();
+    wg_barrier();  // tile it is there, and every wave is done with the one before
+    if (it + NS - 1 < nt) issue(it + NS - 1, next);
     const int kt = bs + it * 64;
-    if (kt + 63 <= tq[0]) tile(std::false_type{}, kt, it & 1);
-    else if (kt <= min(tq[NQ - 1] + 15, be - 1)) tile(std::true_type{}, kt, it & 1);
-    if (it + 2 < nt) {
-      wg_barrier();  // every wave is done with this buffer
-      issue_pair<T, DH, NW>(kb, ldk, vb, ldv, kt + 128, kend - 1, lds[it & 1][0], lds[it & 1][1],
-                            wave, lane);
-    }
+    if (kt + 63 <= tq[0]) tile(std::false_type{}, kt, buf);
+    else if (kt <= min(tq[NQ - 1] + 15, be - 1)) tile(std::true_type{}, kt, buf);
+    buf = buf + 1 == NS ? 0 : buf + 1;
+    next = next + 1 == NS ? 0 : next + 1;
   }
 
   for (int u = dropped; u < min(be, tq[NQ - 1] + 16); ++u)  // (none, as a rule)
@@ -326,6 +347,15 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
   issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs, kend - 1, lds[0][0], lds[0][1], wave, lane);
   if (nt > 1)
     issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + 64, kend - 1, lds[1][0], lds[1][1], wave, lane);
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    settle(ls[nq]);
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) {
+      settle(qf[nq][ds]);
+      settle(df[nq][ds]);
+    }
+  }
   for (int it = 0; it < nt; ++it) {
     if (it + 1 < nt) vm_wait<NI>();
     else vm_wait<0>();
@@ -464,6 +494,13 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
   const ColBase<T> qcol = TL::col_base(lds[0][0], lane), dcol = TL::col_base(lds[0][1], lane);
   issue(0);
   if (nt > 1) issue(1);
+#pragma unroll
+  for (int nk = 0; nk < NK; ++nk)
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) {
+      settle(kf[nk][ds]);
+      settle(vf[nk][ds]);
+    }
   for (int it = 0; it < nt; ++it) {
     if (it + 1 < nt) vm_wait<NI>();
     else vm_wait<0>();
@@ -560,11 +597,16 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
 
 template <typename T, int DH>
 hipError_t fwd_t(const SeqAttn& a, hipStream_t s) {
-  constexpr int NQ = sizeof(T) == 2 ? 2 : 1, QT = 64 * NQ;
-  const int64_t grid = (int64_t)(a.total / QT + a.nseq) * a.H;
-  seq_fwd_kernel<T, DH, NQ><<<dim3((unsigned)grid), 256, 0, s>>>(
-      (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, (T*)a.o, a.lse, a.total, a.nseq, a.H,
-      a.H / a.Hkv, a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e);
+  constexpr int NW = FwdShape<T, DH>::NW, NQ = FwdShape<T, DH>::NQ;
+  const int G = a.H / a.Hkv;
+  // as many heads of a group as divide it: their queries see the same keys
+  int hp = NW;
+  while (G % hp) hp /= 2;
+  const int wph = NW / hp, QT = wph * 16 * NQ;
+  const int64_t grid = (int64_t)(a.total / QT + a.nseq) * (a.H / hp);
+  seq_fwd_kernel<T, DH><<<dim3((unsigned)grid), NW * 64, 0, s>>>(
+      (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, (T*)a.o, a.lse, a.total, a.nseq, a.H, G,
+      wph, a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e);
   return hipGetLastError();
 }
 
@@ -658,6 +700,8 @@ __global__ __launch_bounds__((DecShape<T, DH>::NW * 64)) void dec_part_kernel(De
   int t = t0 + wave, buf = 0;
   if (t < t1) issue(t, 0);
   if (t + NW < t1) issue(t + NW, 1);
+#pragma unroll
+  for (int ds = 0; ds < KS; ++ds) settle(qf[ds]);
   for (; t < t1; t += NW, buf ^= 1) {
     if (t + NW < t1) vm_wait<2 * NI>();
     else vm_wait<0>();
