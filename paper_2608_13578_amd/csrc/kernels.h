@@ -390,12 +390,15 @@ struct SeqAttn {
   const void* dout;
   void *dq, *dk, *dv;  // strides of q, k, v
   float* delta;        // scratch [H, total]
+  float* part;         // scratch [parts, total, Hkv, 2 dh], if there are several parts
   int total, nseq, H, Hkv;
   int64_t ldq, ldk, ldv, ldo;  // ldo: o and dout
   float scale;
 };
 hipError_t seq_attn_fwd(DType dt, int dh, const SeqAttn& a, hipStream_t s);
 hipError_t seq_attn_bwd(DType dt, int dh, const SeqAttn& a, hipStream_t s);
+// Parts in which the gradients of shared heads are summed (1: at once).
+int seq_attn_bwd_parts(DType dt, int dh, int total, int nseq, int Hkv, int G);
 
 // One token per sequence against caches [slots][cap] of Hkv heads.
 struct DecAttn {

@@ -164,7 +164,11 @@ int bcmt_attn_validate(const bcmt_attn_config* cfg) { return check_attn(cfg); }
 
 size_t bcmt_attn_workspace_bytes(const bcmt_attn_config* cfg) {
   if (check_attn(cfg) != BCMT_OK) return 0;
-  return up256((size_t)cfg->H * cfg->total * 4);
+  const bcmt_attn_config& c = *cfg;
+  const int parts =
+      seq_attn_bwd_parts(dtype_of(c.dtype), c.dh, c.total, c.nseq, c.Hkv, c.H / c.Hkv);
+  return up256((size_t)c.H * c.total * 4) +
+         (parts > 1 ? up256((size_t)parts * c.total * c.Hkv * 2 * c.dh * 4) : 0);
 }
 
 int bcmt_attn_forward(const bcmt_attn_config* cfg, const void* q, const void* k, const void* v,
@@ -240,6 +244,7 @@ int bcmt_attn_backward(const bcmt_attn_config* cfg, const void* q, const void* k
   a.dk = dk;
   a.dv = dv;
   a.delta = (float*)ws;
+  a.part = (float*)((char*)ws + up256((size_t)c.H * c.total * 4));
   a.total = c.total;
   a.nseq = c.nseq;
   a.H = c.H;

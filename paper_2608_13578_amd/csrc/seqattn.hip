@@ -70,19 +70,20 @@ __device__ __forceinline__ void issue_pair(const T* a, int64_t lda, const T* b, 
 
 constexpr float kRaise = 8.f;
 
-template <typename T, int DH> struct FwdShape {
-  static constexpr int NW = sizeof(T) == 2 ? 8 : 4, NQ = sizeof(T) == 2 ? 2 : 1;
-  static constexpr int NS = sizeof(T) == 2 ? 4 : DH == 128 ? 2 : 3;
+template <typename T, int DH, int NW_> struct QueryShape {
+  static constexpr int NW = NW_, NQ = sizeof(T) == 2 ? 2 : 1;
+  // buffers of the ring: 128 KB of LDS a workgroup, or 64 KB for two of four waves
+  static constexpr int NS = sizeof(T) == 2 ? (DH == 128 && NW == 4 ? 2 : 4) : DH == 128 ? 2 : 3;
 };
 
-template <typename T, int DH>
-__global__ __launch_bounds__((FwdShape<T, DH>::NW * 64)) void seq_fwd_kernel(
+template <typename T, int DH, int NW>
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_fwd_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const int* __restrict__ cu, T* __restrict__ o, float* __restrict__ lse, int total, int nseq,
     int H, int G, int wph, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
-  constexpr int NW = FwdShape<T, DH>::NW, NQ = FwdShape<T, DH>::NQ, NS = FwdShape<T, DH>::NS;
+  constexpr int NQ = QueryShape<T, DH, NW>::NQ, NS = QueryShape<T, DH, NW>::NS;
   constexpr int KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
   constexpr int NI = kPairLoads<T, DH, NW>;
   constexpr int KUS = sizeof(T) == 2 ? (DH > 64 ? 2 : 4) : 1;  // key groups read at once
@@ -286,22 +287,26 @@ __global__ __launch_bounds__((FwdShape<T, DH>::NW * 64)) void seq_fwd_kernel(
 // The forward's walk again, with delta_t = do_t . o_t formed (and stored for
 // dK/dV) first: s and dp per key tile, dz in place, dQ^T += K^T dZ^T.
 
-template <typename T, int DH, int NQ>
-__global__ __launch_bounds__(256) void seq_dq_kernel(
+template <typename T, int DH, int NW>
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_dq_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const int* __restrict__ cu, const T* __restrict__ o, const float* __restrict__ lse,
     const T* __restrict__ dout, T* __restrict__ dq, float* __restrict__ delta, int total, int nseq,
-    int H, int G, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2, float scale) {
+    int H, int G, int wph, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2,
+    float scale) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
-  constexpr int NW = 4, QT = NW * 16 * NQ, KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
-  constexpr int NI = 2 * TL::NCH / NW;
-  __shared__ __attribute__((aligned(1024))) T lds[2][2][64 * DH];
+  constexpr int NQ = QueryShape<T, DH, NW>::NQ, NS = QueryShape<T, DH, NW>::NS;
+  constexpr int KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
+  constexpr int NI = kPairLoads<T, DH, NW>;
+  constexpr int JB = NJ > 4 ? 4 : NJ;  // column operands read at once
+  __shared__ __attribute__((aligned(1024))) T lds[NS][2][64 * DH];
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
-  const int nslot = total / QT + nseq;
-  const int h = blockIdx.x % H;
-  const SeqTile st = find_tile(cu, nseq, total, QT, nslot - 1 - (int)(blockIdx.x / H));
+  const int QT = wph * 16 * NQ, hp = NW / wph, HG = H / hp;
+  const int nslot = total / QT + nseq, wq = wave % wph;
+  const int h = (int)(blockIdx.x % HG) * hp + wave / wph;
+  const SeqTile st = find_tile(cu, nseq, total, QT, nslot - 1 - (int)(blockIdx.x / HG));
   const int bs = st.begin, be = st.end, q0 = bs + st.tile * QT;
   if (st.tile < 0 || q0 >= be) return;
   const int j = h / G;
@@ -309,9 +314,13 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
   const T* vb = v + j * DH;
   int tq[NQ];
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) tq[nq] = q0 + 16 * (nq & 1 ? 2 * NW - 1 - wave : wave);
+  for (int nq = 0; nq < NQ; ++nq) tq[nq] = q0 + 16 * (nq & 1 ? 2 * wph - 1 - wq : wq);
   const int kend = min(be, q0 + QT);
   const int nt = (kend - bs + 63) / 64;
+  auto issue = [&](int it, int buf) __attribute__((always_inline)) {
+    issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + it * 64, kend - 1, lds[buf][0], lds[buf][1], wave,
+                          lane);
+  };
 
   F qf[NQ][KS], df[NQ][KS];
   float dl[NQ], ls[NQ];
@@ -340,13 +349,73 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
   for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
     for (int jj = 0; jj < NJ; ++jj) da[nq][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+
   constexpr unsigned BUF = 2 * 64 * DH * sizeof(T);
   const unsigned krow = TL::row_base(lds[0][0], lr, lane), vrow = TL::row_base(lds[0][1], lr, lane);
   const ColBase<T> kcol = TL::col_base(lds[0][0], lane);
+  auto tile = [&](auto masked, int kt, int buf) __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(masked)::value;
+    const unsigned ba = buf * BUF;
+    bool live[NQ];
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq)
+      live[nq] = !MASK || !(tq[nq] >= be || tq[nq] + 15 < kt);  // wave-uniform
+    // 32 keys at a time: scores and dp of two key groups, then their part of dQ
+    each<2>([&](auto us) __attribute__((always_inline)) {
+      f32x4 s[NQ][2];
+      each<2>([&](auto k2) __attribute__((always_inline)) {
+        constexpr int ku = us * 2 + k2;
+        RowRaw<T> kr[KS], vr[KS];
+        each<KS>([&](auto ds) {
+          kr[ds] = TL::template row_at<ds, ku * 16>(krow + ba);
+          vr[ds] = TL::template row_at<ds, ku * 16>(vrow + ba);
+        });
+        lds_tr_wait();
+        F kf[KS], vf[KS];
+#pragma unroll
+        for (int ds = 0; ds < KS; ++ds) {
+          kf[ds] = TL::take_row(kr[ds], lane);
+          vf[ds] = TL::take_row(vr[ds], lane);
+        }
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+          f32x4 sv = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) {
+            sv = mma16(kf[ds], qf[nq][ds], sv);
+            dp = mma16(vf[ds], df[nq][ds], dp);
+          }
+          const int t_eff = min(tq[nq] + lr, be - 1);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float z = exp2_fast(fmaf(sv[r], sl2, -ls[nq])) * (dp[r] - dl[nq]);
+            s[nq][k2][r] = !MASK || kt + ku * 16 + lg * 4 + r <= t_eff ? z : 0.f;
+          }
+        }
+      });
+      F zf[NQ];
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) zf[nq] = frag_from<T>(s[nq][0], s[nq][1]);
+      each<NJ / JB>([&](auto jb) __attribute__((always_inline)) {
+        ColRaw<T> kr[JB];
+        each<JB>([&](auto jj) {
+          kr[jj] = TL::template col_at<jb * JB + jj, us * 32, us * 32 + 16>(kcol, ba);
+        });
+        lds_tr_wait();
+#pragma unroll
+        for (int jj = 0; jj < JB; ++jj) {
+          const F kc = take(kr[jj]);
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq)
+            if (live[nq]) da[nq][jb * JB + jj] = mma16(kc, zf[nq], da[nq][jb * JB + jj]);
+        }
+      });
+    });
+  };
 
-  issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs, kend - 1, lds[0][0], lds[0][1], wave, lane);
-  if (nt > 1)
-    issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + 64, kend - 1, lds[1][0], lds[1][1], wave, lane);
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (i < nt) issue(i, i);
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
     settle(ls[nq]);
@@ -356,71 +425,17 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
       settle(df[nq][ds]);
     }
   }
+  int buf = 0, next = NS - 1;
   for (int it = 0; it < nt; ++it) {
-    if (it + 1 < nt) vm_wait<NI>();
+    if (it + NS - 2 < nt) vm_wait<(NS - 2) * NI>();
     else vm_wait<0>();
-    wg_barrier();
+    wg_barrier();  // tile it is there, and every wave is done with the one before
+    if (it + NS - 1 < nt) issue(it + NS - 1, next);
     const int kt = bs + it * 64;
-    const unsigned ba = (it & 1) * BUF;
-    bool live[NQ], any = false;
-#pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) {
-      live[nq] = !(tq[nq] >= be || tq[nq] + 15 < kt);  // wave-uniform
-      any |= live[nq];
-    }
-    if (any) {
-      // 32 keys at a time: scores and dp of two key groups, then their part of dQ
-      each<2>([&](auto us) __attribute__((always_inline)) {
-        f32x4 s[NQ][2];
-        each<2>([&](auto k2) __attribute__((always_inline)) {
-          constexpr int ku = us * 2 + k2;
-          RowRaw<T> kr[KS], vr[KS];
-          each<KS>([&](auto ds) {
-            kr[ds] = TL::template row_at<ds, ku * 16>(krow + ba);
-            vr[ds] = TL::template row_at<ds, ku * 16>(vrow + ba);
-          });
-          lds_tr_wait();
-          F kf[KS], vf[KS];
-#pragma unroll
-          for (int ds = 0; ds < KS; ++ds) {
-            kf[ds] = TL::take_row(kr[ds], lane);
-            vf[ds] = TL::take_row(vr[ds], lane);
-          }
-#pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) {
-            f32x4 sv = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ds = 0; ds < KS; ++ds) {
-              sv = mma16(kf[ds], qf[nq][ds], sv);
-              dp = mma16(vf[ds], df[nq][ds], dp);
-            }
-            const int t_eff = min(tq[nq] + lr, be - 1);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int u = kt + ku * 16 + lg * 4 + r;
-              s[nq][k2][r] =
-                  u <= t_eff ? exp2_fast(sv[r] * sl2 - ls[nq]) * (dp[r] - dl[nq]) : 0.f;
-            }
-          }
-        });
-        F zf[NQ];
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) zf[nq] = frag_from<T>(s[nq][0], s[nq][1]);
-        each<NJ>([&](auto jj) __attribute__((always_inline)) {
-          ColRaw<T> kr = TL::template col_at<jj, us * 32, us * 32 + 16>(kcol, ba);
-          lds_tr_wait();
-          const F kc = take(kr);
-#pragma unroll
-          for (int nq = 0; nq < NQ; ++nq)
-            if (live[nq]) da[nq][jj] = mma16(kc, zf[nq], da[nq][jj]);
-        });
-      });
-    }
-    if (it + 2 < nt) {
-      wg_barrier();
-      issue_pair<T, DH, NW>(kb, ldk, vb, ldv, kt + 128, kend - 1, lds[it & 1][0], lds[it & 1][1],
-                            wave, lane);
-    }
+    if (kt + 63 <= tq[0]) tile(std::false_type{}, kt, buf);
+    else if (kt <= min(tq[NQ - 1] + 15, be - 1)) tile(std::true_type{}, kt, buf);
+    buf = buf + 1 == NS ? 0 : buf + 1;
+    next = next + 1 == NS ? 0 : next + 1;
   }
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
@@ -436,31 +451,47 @@ __global__ __launch_bounds__(256) void seq_dq_kernel(
 }
 
 // ------------------------------------------------------------------ backward: dK, dV
-// One workgroup of four waves: 64 NK keys of one key/value head, NK groups of
-// 16 per wave.  It walks the query tiles at or after its keys, for every query
-// head of the group in turn, so that shared heads are summed in registers in
-// a fixed order.
+// A workgroup owns 64 NK keys of one key/value head and walks the steps (query
+// head of the group, tile of 64 queries at or after its keys).  NH teams of four
+// waves take the steps in turn and are joined at the end, so that a SIMD has
+// two waves and the keys with the most queries behind them are done sooner.
+// Shared heads are summed in registers, in a fixed order; where there are too
+// few workgroups for the chip, each takes a part of the group's heads and leaves
+// float32 sums that a second kernel adds.
 
-template <typename T, int DH, int NK>
-__global__ __launch_bounds__(256) void seq_dkdv_kernel(
+template <typename T, int DH> struct KeyShape {
+  static constexpr int NK = sizeof(T) == 2 ? 2 : 1;  // groups of 16 keys of a wave
+  static constexpr int NH = sizeof(T) * DH > 128 ? 1 : 2;
+  static constexpr int NS = sizeof(T) * DH >= 512 ? 2 : 3;  // buffers of the ring
+};
+
+template <typename T, int DH>
+__global__ __launch_bounds__((KeyShape<T, DH>::NH * 256)) void seq_dkdv_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const int* __restrict__ cu, const float* __restrict__ lse, const float* __restrict__ delta,
-    const T* __restrict__ dout, T* __restrict__ dk, T* __restrict__ dv, int total, int nseq, int H,
-    int G, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2, float scale) {
+    const T* __restrict__ dout, T* __restrict__ dk, T* __restrict__ dv, float* __restrict__ part,
+    int parts, int total, int nseq, int H, int G, int64_t ldq, int64_t ldk, int64_t ldv,
+    int64_t ldo, float sl2, float scale) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
+  constexpr int NK = KeyShape<T, DH>::NK, NH = KeyShape<T, DH>::NH, NS = KeyShape<T, DH>::NS;
   constexpr int NW = 4, KT = NW * 16 * NK, KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
-  constexpr int NI = 2 * TL::NCH / NW + 1;
-  __shared__ __attribute__((aligned(1024))) T lds[2][2][64 * DH];
-  __shared__ __attribute__((aligned(16))) float rows[2][NW][64];  // lse, delta: waves 0 and 1
-  const int lane = threadIdx.x & 63, wave = wave_index();
+  constexpr int NI = kPairLoads<T, DH, NW> + 1;
+  constexpr int JB = sizeof(T) == 2 ? NJ : NJ > 2 ? 2 : NJ;  // column operands read at once
+  constexpr int RING = NS * NH * 2 * 64 * DH, JOIN = NH > 1 ? 2 * NW * NK * NJ * 64 * 4 : 0;
+  constexpr int LDS = RING * (int)sizeof(T) > JOIN * 4 ? RING : JOIN * 4 / (int)sizeof(T);
+  __shared__ __attribute__((aligned(1024))) T lds[LDS];
+  __shared__ __attribute__((aligned(16))) float rows[NS][NH][NW][64];  // lse, delta: waves 0, 1
+  const int lane = threadIdx.x & 63, wave = wave_index() % NW, team = wave_index() / NW;
   const int lr = lane & 15, lg = lane >> 4;
   const int Hkv = H / G;
-  const int j = blockIdx.x % Hkv;
-  const SeqTile st = find_tile(cu, nseq, total, KT, (int)(blockIdx.x / Hkv));
+  const int j = blockIdx.x % Hkv, pt = blockIdx.x / Hkv % parts;
+  const SeqTile st = find_tile(cu, nseq, total, KT, (int)(blockIdx.x / (Hkv * parts)));
   const int be = st.end, k0 = st.begin + st.tile * KT;
   if (st.tile < 0 || k0 >= be) return;
-  const int nt1 = (be - k0 + 63) / 64, nt = nt1 * G;  // query tiles of a head, of all
+  const int heads = G / parts, h0 = j * G + pt * heads;
+  const int nt1 = (be - k0 + 63) / 64, nstep = nt1 * heads;  // query tiles of a head, of all
+  const int nt = (nstep + NH - 1) / NH;
 
   int uk[NK];
   F kf[NK][KS], vf[NK][KS];
@@ -481,19 +512,101 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
       va[nk][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
   }
-  auto issue = [&](int it) {
-    const int h = j * G + it / nt1, tt = k0 + (it % nt1) * 64;
-    issue_pair<T, DH, NW>(q + h * DH, ldq, dout + h * DH, ldo, tt, be - 1, lds[it & 1][0],
-                          lds[it & 1][1], wave, lane);
+  constexpr int TILE = 64 * DH;
+  // step it NH + team into a buffer (beyond the last step: the last one again)
+  auto issue = [&](int it, int buf) __attribute__((always_inline)) {
+    const int step = min(it * NH + team, nstep - 1);
+    const int h = h0 + step / nt1, tt = k0 + (step % nt1) * 64;
+    T* t = lds + (buf * NH + team) * 2 * TILE;
+    issue_pair<T, DH, NW>(q + h * DH, ldq, dout + h * DH, ldo, tt, be - 1, t, t + TILE, wave, lane);
     const float* src = (wave & 1 ? delta : lse) + (int64_t)h * total + min(tt + lane, be - 1);
-    __builtin_amdgcn_global_load_lds(src, (lds_void_t*)rows[it & 1][wave], 4, 0, 0);
+    __builtin_amdgcn_global_load_lds(src, (lds_void_t*)rows[buf][team][wave], 4, 0, 0);
+  };
+  constexpr unsigned BUF = NH * 2 * TILE * sizeof(T);
+  T* mine = lds + team * 2 * TILE;
+  const unsigned qrow = TL::row_base(mine, lr, lane), drow = TL::row_base(mine + TILE, lr, lane);
+  const ColBase<T> qcol = TL::col_base(mine, lane), dcol = TL::col_base(mine + TILE, lane);
+  const unsigned lrow = lds_addr(&rows[0][team][0][lg * 4]);
+  const unsigned dlrow = lds_addr(&rows[0][team][1][lg * 4]);
+
+  auto tile = [&](auto masked, int tt, int buf) __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(masked)::value;
+    const unsigned ba = buf * BUF, br = buf * (NH * NW * 64 * 4);
+    bool live[NK];
+#pragma unroll
+    for (int nk = 0; nk < NK; ++nk)
+      live[nk] = !MASK || !(uk[nk] >= be || tt + 63 < uk[nk]);  // wave-uniform
+    // 32 queries at a time
+    each<2>([&](auto us) __attribute__((always_inline)) {
+      f32x4 p[NK][2], z[NK][2];
+      each<2>([&](auto t2) __attribute__((always_inline)) {
+        constexpr int ts = us * 2 + t2;
+        RowRaw<T> qr[KS], dr[KS];
+        each<KS>([&](auto ds) {
+          qr[ds] = TL::template row_at<ds, ts * 16>(qrow + ba);
+          dr[ds] = TL::template row_at<ds, ts * 16>(drow + ba);
+        });
+        f32x4 ls = lds_read_f32x4_at<ts * 64>(lrow + br);
+        f32x4 dl = lds_read_f32x4_at<ts * 64>(dlrow + br);
+        lds_tr_wait();
+        F qf[KS], df[KS];
+#pragma unroll
+        for (int ds = 0; ds < KS; ++ds) {
+          qf[ds] = TL::take_row(qr[ds], lane);
+          df[ds] = TL::take_row(dr[ds], lane);
+        }
+        lds_tr_bind(ls);
+        lds_tr_bind(dl);
+        ls *= -kLog2e;
+#pragma unroll
+        for (int nk = 0; nk < NK; ++nk) {
+          f32x4 sv = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) {
+            sv = mma16(qf[ds], kf[nk][ds], sv);
+            dp = mma16(df[ds], vf[nk][ds], dp);
+          }
+          const int u = uk[nk] + lr;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float pv = exp2_fast(fmaf(sv[r], sl2, ls[r])), zv = pv * (dp[r] - dl[r]);
+            const int t = tt + ts * 16 + lg * 4 + r;
+            const bool ok = !MASK || (t >= u && t < be);
+            p[nk][t2][r] = ok ? pv : 0.f;
+            z[nk][t2][r] = ok ? zv : 0.f;
+          }
+        }
+      });
+      F pf[NK], zf[NK];
+#pragma unroll
+      for (int nk = 0; nk < NK; ++nk) {
+        pf[nk] = frag_from<T>(p[nk][0], p[nk][1]);
+        zf[nk] = frag_from<T>(z[nk][0], z[nk][1]);
+      }
+      each<NJ / JB>([&](auto jb) __attribute__((always_inline)) {
+        ColRaw<T> dr[JB], qr[JB];
+        each<JB>([&](auto jj) {
+          dr[jj] = TL::template col_at<jb * JB + jj, us * 32, us * 32 + 16>(dcol, ba);
+          qr[jj] = TL::template col_at<jb * JB + jj, us * 32, us * 32 + 16>(qcol, ba);
+        });
+        lds_tr_wait();
+#pragma unroll
+        for (int jj = 0; jj < JB; ++jj) {
+          const F dc = take(dr[jj]), qc = take(qr[jj]);
+#pragma unroll
+          for (int nk = 0; nk < NK; ++nk)
+            if (live[nk]) {
+              va[nk][jb * JB + jj] = mma16(dc, pf[nk], va[nk][jb * JB + jj]);
+              ka[nk][jb * JB + jj] = mma16(qc, zf[nk], ka[nk][jb * JB + jj]);
+            }
+        }
+      });
+    });
   };
 
-  constexpr unsigned BUF = 2 * 64 * DH * sizeof(T);
-  const unsigned qrow = TL::row_base(lds[0][0], lr, lane), drow = TL::row_base(lds[0][1], lr, lane);
-  const ColBase<T> qcol = TL::col_base(lds[0][0], lane), dcol = TL::col_base(lds[0][1], lane);
-  issue(0);
-  if (nt > 1) issue(1);
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (i < nt) issue(i, i);
 #pragma unroll
   for (int nk = 0; nk < NK; ++nk)
 #pragma unroll
@@ -501,88 +614,55 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
       settle(kf[nk][ds]);
       settle(vf[nk][ds]);
     }
+  int buf = 0, next = NS - 1;
   for (int it = 0; it < nt; ++it) {
-    if (it + 1 < nt) vm_wait<NI>();
+    if (it + NS - 2 < nt) vm_wait<(NS - 2) * NI>();
     else vm_wait<0>();
-    wg_barrier();
-    const int tt = k0 + (it % nt1) * 64;
-    const unsigned ba = (it & 1) * BUF;
-    bool live[NK], any = false;
-#pragma unroll
-    for (int nk = 0; nk < NK; ++nk) {
-      live[nk] = !(uk[nk] >= be || tt + 63 < uk[nk]);  // wave-uniform
-      any |= live[nk];
+    wg_barrier();  // the steps it NH .. are there, and every wave is done with those before
+    if (it + NS - 1 < nt) issue(it + NS - 1, next);
+    const int step = it * NH + team, tt = k0 + (step % nt1) * 64;
+    if (step < nstep && uk[0] < be) {
+      if (tt >= uk[NK - 1] + 15 && tt + 64 <= be) tile(std::false_type{}, tt, buf);
+      else if (tt + 63 >= uk[0]) tile(std::true_type{}, tt, buf);
     }
-    if (any) {
-      // 32 queries at a time
-      each<2>([&](auto us) __attribute__((always_inline)) {
-        f32x4 p[NK][2], z[NK][2];
-        each<2>([&](auto t2) __attribute__((always_inline)) {
-          constexpr int ts = us * 2 + t2;
-          RowRaw<T> qr[KS], dr[KS];
-          each<KS>([&](auto ds) {
-            qr[ds] = TL::template row_at<ds, ts * 16>(qrow + ba);
-            dr[ds] = TL::template row_at<ds, ts * 16>(drow + ba);
-          });
-          f32x4 ls = lds_read_f32x4(&rows[it & 1][0][ts * 16 + lg * 4]);
-          f32x4 dl = lds_read_f32x4(&rows[it & 1][1][ts * 16 + lg * 4]);
-          lds_tr_wait();
-          F qf[KS], df[KS];
+    buf = buf + 1 == NS ? 0 : buf + 1;
+    next = next + 1 == NS ? 0 : next + 1;
+  }
+  if constexpr (NH > 1) {
+    wg_barrier();  // every wave is done with the ring
+    f32x4* join = (f32x4*)lds;
+    if (team == 1) {
 #pragma unroll
-          for (int ds = 0; ds < KS; ++ds) {
-            qf[ds] = TL::take_row(qr[ds], lane);
-            df[ds] = TL::take_row(dr[ds], lane);
-          }
-          lds_tr_bind(ls);
-          lds_tr_bind(dl);
+      for (int nk = 0; nk < NK; ++nk)
 #pragma unroll
-          for (int nk = 0; nk < NK; ++nk) {
-            f32x4 sv = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ds = 0; ds < KS; ++ds) {
-              sv = mma16(qf[ds], kf[nk][ds], sv);
-              dp = mma16(df[ds], vf[nk][ds], dp);
-            }
-            const int u = uk[nk] + lr;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int t = tt + ts * 16 + lg * 4 + r;
-              const bool ok = t >= u && t < be;
-              const float pv = ok ? exp2_fast(sv[r] * sl2 - ls[r] * kLog2e) : 0.f;
-              p[nk][t2][r] = pv;
-              z[nk][t2][r] = ok ? pv * (dp[r] - dl[r]) : 0.f;
-            }
-          }
-        });
-        F pf[NK], zf[NK];
-#pragma unroll
-        for (int nk = 0; nk < NK; ++nk) {
-          pf[nk] = frag_from<T>(p[nk][0], p[nk][1]);
-          zf[nk] = frag_from<T>(z[nk][0], z[nk][1]);
+        for (int jj = 0; jj < NJ; ++jj) {
+          join[((wave * NK + nk) * NJ + jj) * 64 + lane] = ka[nk][jj];
+          join[(((NW + wave) * NK + nk) * NJ + jj) * 64 + lane] = va[nk][jj];
         }
-        each<NJ>([&](auto jj) __attribute__((always_inline)) {
-          ColRaw<T> dr = TL::template col_at<jj, us * 32, us * 32 + 16>(dcol, ba);
-          ColRaw<T> qr = TL::template col_at<jj, us * 32, us * 32 + 16>(qcol, ba);
-          lds_tr_wait();
-          const F dc = take(dr), qc = take(qr);
+    }
+    __syncthreads();
+    if (team == 1) return;
 #pragma unroll
-          for (int nk = 0; nk < NK; ++nk)
-            if (live[nk]) {
-              va[nk][jj] = mma16(dc, pf[nk], va[nk][jj]);
-              ka[nk][jj] = mma16(qc, zf[nk], ka[nk][jj]);
-            }
-        });
-      });
-    }
-    if (it + 2 < nt) {
-      wg_barrier();
-      issue(it + 2);
-    }
+    for (int nk = 0; nk < NK; ++nk)
+#pragma unroll
+      for (int jj = 0; jj < NJ; ++jj) {
+        ka[nk][jj] += join[((wave * NK + nk) * NJ + jj) * 64 + lane];
+        va[nk][jj] += join[(((NW + wave) * NK + nk) * NJ + jj) * 64 + lane];
+      }
   }
 #pragma unroll
   for (int nk = 0; nk < NK; ++nk) {
     const int u = uk[nk] + lr;
     if (u < be) {
+      if (parts > 1) {
+        float* p = part + (((int64_t)pt * total + u) * Hkv + j) * 2 * DH + lg * 4;
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) {
+          *(f32x4*)(p + jj * 16) = ka[nk][jj] * scale;
+          *(f32x4*)(p + DH + jj * 16) = va[nk][jj];
+        }
+        continue;
+      }
       T* pk = dk + (int64_t)u * ldk + j * DH + lg * 4;
       T* pv = dv + (int64_t)u * ldv + j * DH + lg * 4;
 #pragma unroll
@@ -595,37 +675,104 @@ __global__ __launch_bounds__(256) void seq_dkdv_kernel(
   }
 }
 
+// dK and dV of the rows of all sequences from the parts of their heads: DH / 2
+// threads a row and head, four values each.
 template <typename T, int DH>
-hipError_t fwd_t(const SeqAttn& a, hipStream_t s) {
-  constexpr int NW = FwdShape<T, DH>::NW, NQ = FwdShape<T, DH>::NQ;
-  const int G = a.H / a.Hkv;
-  // as many heads of a group as divide it: their queries see the same keys
+__global__ __launch_bounds__(256) void seq_dkdv_sum_kernel(const int* __restrict__ cu,
+                                                           const float* __restrict__ part,
+                                                           int parts, T* __restrict__ dk,
+                                                           T* __restrict__ dv, int total, int nseq,
+                                                           int Hkv, int64_t ldk, int64_t ldv) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)total * Hkv * (DH / 2);
+  if (i >= n) return;
+  const int c = (int)(i % (DH / 2)) * 4;
+  const int64_t r = i / (DH / 2);
+  const int j = (int)(r % Hkv), u = (int)(r / Hkv);
+  if (u < cu[0] || u >= cu[nseq]) return;
+  f32x4 s = *(const f32x4*)(part + r * 2 * DH + c);
+  for (int p = 1; p < parts; ++p)
+    s += *(const f32x4*)(part + ((int64_t)p * total * Hkv + r) * 2 * DH + c);
+  if (c < DH) store4(dk + (int64_t)u * ldk + j * DH + c, s[0], s[1], s[2], s[3]);
+  else store4(dv + (int64_t)u * ldv + j * DH + c - DH, s[0], s[1], s[2], s[3]);
+}
+
+// Waves per head of a workgroup of NW: as many heads of a group share it as
+// divide the group, since their queries see the same keys.
+int waves_per_head(int NW, int G) {
   int hp = NW;
   while (G % hp) hp /= 2;
-  const int wph = NW / hp, QT = wph * 16 * NQ;
-  const int64_t grid = (int64_t)(a.total / QT + a.nseq) * (a.H / hp);
-  seq_fwd_kernel<T, DH><<<dim3((unsigned)grid), NW * 64, 0, s>>>(
+  return NW / hp;
+}
+int64_t query_grid(int NW, int NQ, const SeqAttn& a) {
+  const int wph = waves_per_head(NW, a.H / a.Hkv);
+  return (int64_t)(a.total / (wph * 16 * NQ) + a.nseq) * (a.H * wph / NW);
+}
+// Eight waves a workgroup (less traffic per query) once they make four rounds
+// over the CUs, else four.
+bool wide_queries(DType dt, const SeqAttn& a) {
+  return dt == DType::BF16 && query_grid(8, 2, a) >= 1024;
+}
+
+template <typename T, int DH, int NW>
+hipError_t fwd_nw(const SeqAttn& a, hipStream_t s) {
+  const int64_t grid = query_grid(NW, QueryShape<T, DH, NW>::NQ, a);
+  const int G = a.H / a.Hkv;
+  seq_fwd_kernel<T, DH, NW><<<dim3((unsigned)grid), NW * 64, 0, s>>>(
       (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, (T*)a.o, a.lse, a.total, a.nseq, a.H, G,
-      wph, a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e);
+      waves_per_head(NW, G), a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e);
+  return hipGetLastError();
+}
+template <typename T, int DH, int NW>
+hipError_t dq_nw(const SeqAttn& a, hipStream_t s) {
+  const int64_t grid = query_grid(NW, QueryShape<T, DH, NW>::NQ, a);
+  const int G = a.H / a.Hkv;
+  seq_dq_kernel<T, DH, NW><<<dim3((unsigned)grid), NW * 64, 0, s>>>(
+      (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, (const T*)a.o, a.lse, (const T*)a.dout,
+      (T*)a.dq, a.delta, a.total, a.nseq, a.H, G, waves_per_head(NW, G), a.ldq, a.ldk, a.ldv, a.ldo,
+      a.scale * kLog2e, a.scale);
   return hipGetLastError();
 }
 
 template <typename T, int DH>
+hipError_t fwd_t(const SeqAttn& a, hipStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (wide_queries(DType::BF16, a)) return fwd_nw<T, DH, 8>(a, s);
+  return fwd_nw<T, DH, 4>(a, s);
+}
+
+// Parts of a group's heads for dK and dV: a divisor of G, until there are two
+// workgroups for every CU.
+int head_parts(int64_t tiles, int Hkv, int G) {
+  int p = 1;
+  while (p < G && (G % p || tiles * Hkv * p < 512)) ++p;
+  return p;
+}
+template <typename T, int DH>
+int parts_t(int total, int nseq, int Hkv, int G) {
+  return head_parts(total / (64 * KeyShape<T, DH>::NK) + nseq, Hkv, G);
+}
+
+template <typename T, int DH>
 hipError_t bwd_t(const SeqAttn& a, hipStream_t s) {
-  constexpr int NQ = sizeof(T) == 2 ? 2 : 1, QT = 64 * NQ;
   const int G = a.H / a.Hkv;
-  const int64_t gq = (int64_t)(a.total / QT + a.nseq) * a.H;
-  seq_dq_kernel<T, DH, NQ><<<dim3((unsigned)gq), 256, 0, s>>>(
-      (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, (const T*)a.o, a.lse, (const T*)a.dout,
-      (T*)a.dq, a.delta, a.total, a.nseq, a.H, G, a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e,
-      a.scale);
-  hipError_t e = hipGetLastError();
+  hipError_t e;
+  if constexpr (sizeof(T) == 2)
+    e = wide_queries(DType::BF16, a) ? dq_nw<T, DH, 8>(a, s) : dq_nw<T, DH, 4>(a, s);
+  else
+    e = dq_nw<T, DH, 4>(a, s);
   if (e != hipSuccess) return e;
-  const int64_t gk = (int64_t)(a.total / QT + a.nseq) * a.Hkv;
-  seq_dkdv_kernel<T, DH, NQ><<<dim3((unsigned)gk), 256, 0, s>>>(
+  constexpr int KT = 64 * KeyShape<T, DH>::NK;
+  const int parts = parts_t<T, DH>(a.total, a.nseq, a.Hkv, G);
+  const int64_t grid = (int64_t)(a.total / KT + a.nseq) * a.Hkv * parts;
+  seq_dkdv_kernel<T, DH><<<dim3((unsigned)grid), KeyShape<T, DH>::NH * 256, 0, s>>>(
       (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, a.lse, a.delta, (const T*)a.dout,
-      (T*)a.dk, (T*)a.dv, a.total, a.nseq, a.H, G, a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e,
-      a.scale);
+      (T*)a.dk, (T*)a.dv, a.part, parts, a.total, a.nseq, a.H, G, a.ldq, a.ldk, a.ldv, a.ldo,
+      a.scale * kLog2e, a.scale);
+  e = hipGetLastError();
+  if (e != hipSuccess || parts == 1) return e;
+  const int64_t n = (int64_t)a.total * a.Hkv * (DH / 2);
+  seq_dkdv_sum_kernel<T, DH><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(
+      a.cu, a.part, parts, (T*)a.dk, (T*)a.dv, a.total, a.nseq, a.Hkv, a.ldk, a.ldv);
   return hipGetLastError();
 }
 
@@ -865,6 +1012,9 @@ hipError_t seq_attn_fwd(DType dt, int dh, const SeqAttn& a, hipStream_t s) {
 }
 hipError_t seq_attn_bwd(DType dt, int dh, const SeqAttn& a, hipStream_t s) {
   BY_TYPE_AND_WIDTH(bwd_t, dt, dh, a, s);
+}
+int seq_attn_bwd_parts(DType dt, int dh, int total, int nseq, int Hkv, int G) {
+  BY_TYPE_AND_WIDTH(parts_t, dt, dh, total, nseq, Hkv, G);
 }
 hipError_t seq_attn_decode(DType dt, int dh, const DecAttn& a, hipStream_t s) {
   BY_TYPE_AND_WIDTH(dec_t, dt, dh, a, s);
