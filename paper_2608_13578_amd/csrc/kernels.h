@@ -428,12 +428,13 @@ struct LinPass {
   int total, nseq, H, seg;  // seg: rows of a segment, a multiple of 64
   int64_t lda, ldb, ldc, ldo;
   float s_intra, s_inter, s_upd;  // factors of the scores, of the state's term, of its update
+  bool fine;  // the state can be an output: sums of 24 bits, not 16
 };
 // state: only the segments' own sums -> seg_state (rows b, columns c).
 hipError_t lin_pass(DType dt, int dh, const LinPass& a, bool rev, bool state, hipStream_t s);
 // Those sums -> the states at the boundaries between segments (s_in unswapped).
 hipError_t lin_scan(int dh, const LinPass& a, bool rev, hipStream_t s);
-int lin_segment_rows(int total, int H);
+int lin_segment_rows(int total, int nseq, int H, int dh);
 
 struct LinDecay {
   const void *q, *k, *v, *dout;

@@ -23,7 +23,8 @@
 // decayed scores of a chunk are shared through LDS.
 //
 // The sum of a state takes its weighted rows g^n c_j in three bf16 parts
-// (24 bits), so that a float32 state loses nothing to bf16 products; scores and
+// (24 bits) where the float32 state can be an output, so that it loses nothing to
+// bf16 products, and in two (16 bits) where only bf16 outputs read it; scores and
 // the state as an operand of a bf16 output are rounded to bf16 once, an error
 // below the output's own rounding.
 //
@@ -45,22 +46,26 @@ __device__ __forceinline__ float powg(float lg2, int e) {  // g^e; 0^0 = 1
   return e == 0 ? 1.f : exp2_fast(lg2 * (float)e);
 }
 
-template <typename T> struct Parts;  // exact enough operands of a float32 sum
+// x as a sum of operands of the type: one in float32, three in bf16 (24 bits; the
+// third only if `fine`).
+template <typename T> struct Parts;
 template <> struct Parts<float> { static constexpr int N = 1; };
 template <> struct Parts<bf16> { static constexpr int N = 3; };
 
-__device__ __forceinline__ void split(const float (&x)[8], f32x8 (&p)[1]) {
+__device__ __forceinline__ void split(const float (&x)[8], f32x8 (&p)[1], bool) {
   p[0] = f32x8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
 }
-__device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&p)[3]) {
+__device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&p)[3], bool fine) {
+  float r[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const bf16 a = (bf16)x[e];
-    const float r = x[e] - (float)a;
-    const bf16 b = (bf16)r;
-    p[0][e] = a;
-    p[1][e] = b;
-    p[2][e] = (bf16)(r - (float)b);
+    p[0][e] = (bf16)x[e];
+    r[e] = x[e] - (float)p[0][e];
+    p[1][e] = (bf16)r[e];
+  }
+  if (fine) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[2][e] = (bf16)(r[e] - (float)p[1][e]);
   }
 }
 
@@ -89,27 +94,36 @@ __device__ __forceinline__ typename Frag<T>::type take_row8p(HalfRaw<T>& r) {
 }
 
 // state += (rows a)^T (weighted rows c): this wave's 16 columns, the 64 rows
-// of a chunk.  w: weights of the 8 rows lane / 16 holds in each half chunk; a
-// zero weight drops its row whatever it holds.
-template <typename T, int DH>
-__device__ __forceinline__ void add_outer(f32x4 (&S)[DH / 16], const T* At,
+// of a chunk.  w: weights of the 8 rows lane / 16 holds in each half chunk.
+template <typename T, int DH, int TB_ = DH / 16>
+__device__ __forceinline__ void add_outer(f32x4 (&S)[DH / 16], const ColBase<T>& abase, unsigned add,
                                           const typename Frag<T>::type (&cf)[2],
-                                          const float (&w)[2][8], int lane) {
+                                          const float (&w)[2][8], bool fine) {
   typedef typename Frag<T>::type F;
-  constexpr int NP = Parts<T>::N;
-  const ColBase<T> base = Tile<T, DH>::col_base(At, lane);
+  constexpr int NP = Parts<T>::N, NT = DH / 16, TB = sizeof(T) == 2 || NT < 2 ? (TB_ < NT ? TB_ : NT) : 2;
   each<2>([&](auto us) __attribute__((always_inline)) {
-    float x[8];
+    each<NT / TB>([&](auto tb) __attribute__((always_inline)) {
+      ColRaw<T> ar[TB];
+      each<TB>([&](auto t) {
+        ar[t] = Tile<T, DH>::template col_at<tb * TB + t, us * 32, us * 32 + 16>(abase, add);
+      });
+      F p[NP];
+      float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = w[us][e] == 0.f ? 0.f : w[us][e] * to_f32(cf[us][e]);
-    F p[NP];
-    split(x, p);
-    each<DH / 16>([&](auto t) __attribute__((always_inline)) {
-      ColRaw<T> ar = Tile<T, DH>::template col_at<t, us * 32, us * 32 + 16>(base, 0);
+      for (int e = 0; e < 8; ++e) x[e] = w[us][e] * to_f32(cf[us][e]);
+      split(x, p, fine);
       lds_tr_wait();
-      const F a = take(ar);
+      F a[TB];
 #pragma unroll
-      for (int n = NP - 1; n >= 0; --n) S[t] = mma16(a, p[n], S[t]);
+      for (int t = 0; t < TB; ++t) a[t] = take(ar[t]);
+      if (NP == 3 && fine) {
+#pragma unroll
+        for (int t = 0; t < TB; ++t) S[tb * TB + t] = mma16(a[t], p[NP - 1], S[tb * TB + t]);
+      }
+#pragma unroll
+      for (int n = NP == 3 ? 1 : 0; n >= 0; --n)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) S[tb * TB + t] = mma16(a[t], p[n], S[tb * TB + t]);
     });
   });
 }
@@ -155,6 +169,15 @@ __device__ __forceinline__ LinSeg lin_segment(const int* cu, int nseq, int total
   return r;
 }
 
+// Buffers of the chunks' tiles: as many as give two workgroups of a CU (one of
+// 128-wide heads) their LDS.  A chunk takes less time than its rows take to come
+// from memory, so two chunks are requested ahead.
+template <typename T, int DH>
+constexpr int lin_buffers(bool state) {
+  const int row = (int)sizeof(T) * DH;
+  return state ? (row > 256 ? 2 : row == 256 ? 4 : 3) : row > 256 ? 1 : sizeof(T) == 4 && DH >= 32 ? 2 : 3;
+}
+
 // ------------------------------------------------------------------ the operator
 // REV: rows in reverse.  STATE: only the segment's own sum of states.
 
@@ -164,15 +187,18 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
   typedef Tile<T, DH> TL;
   typedef Tile<T, kC> TP;
   constexpr int NW = DH / 16, NT = DH / 16, KS = DH >= 32 ? DH / 32 : 1;
-  constexpr int NB = sizeof(T) * DH > 256 ? 1 : 2;  // buffers: LDS of three tiles each
-  constexpr int FIRST = STATE ? 1 : 0;              // tiles a, b, c: the sum needs b and c
+  constexpr int FIRST = STATE ? 1 : 0;  // tiles a, b, c: the sum needs b and c
+  constexpr int NB = lin_buffers<T, DH>(STATE);
   constexpr int NI = TL::NCH / NW;  // loads of a tile by each wave
   __shared__ __attribute__((aligned(1024))) T lds[NB][3 - FIRST][kC * DH];
   __shared__ __attribute__((aligned(1024))) T P[STATE ? 16 : kC * kC];
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int h = blockIdx.x % a.H;
-  const LinSeg sg = lin_segment(a.cu, a.nseq, a.total, a.seg, blockIdx.x / a.H);
+  // The pass over the segments' sums walks them in order, the operator backwards:
+  // it begins with the rows that were read last and are still in the cache.
+  const int slot = blockIdx.x / a.H, nslot = a.total / a.seg + a.nseq;
+  const LinSeg sg = lin_segment(a.cu, a.nseq, a.total, a.seg, STATE ? slot : nslot - 1 - slot);
   if (sg.len < 0) return;
   // the sum of a segment that no other follows is not needed
   if (STATE && (REV ? sg.t0 == 0 : sg.last)) return;
@@ -197,8 +223,7 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
   const T* A = STATE ? nullptr : (const T*)a.a + r0 * a.lda + h * DH;
   const T* B = (const T*)a.b + r0 * a.ldb + h * DH;
   const T* Cc = (const T*)a.c + r0 * a.ldc + h * DH;
-  auto issue = [=](int c) __attribute__((always_inline)) {
-    const int buf = NB == 2 ? c & 1 : 0;
+  auto issue = [=](int c, int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int ti = wave * NI + i;
@@ -225,48 +250,69 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
   for (int ib = 0; ib < 4; ++ib) fi[ib] = a.s_inter * powg(lg2, ib * 16 + lr + EI);
   const float gC = powg(lg2, kC);
 
-  // this wave's columns of a tile: the column operand 16 wave .. + 15
-  auto own_cols = [&](ColRaw<T>(&r)[2], const T* t) __attribute__((always_inline)) {
-    ColBase<T> b = TL::col_base(t, lane);
-    for (auto& x : b.a) x ^= wave * 16 * (int)sizeof(T);
-    each<2>([&](auto us) { r[us] = TL::template col_at<0, us * 32, us * 32 + 16>(b, 0); });
-  };
-  if (NB == 2 && nc > 0) issue(0);
+  // The scores of a chunk: 16 x 16 blocks (ib, jb), jb <= ib, and the zero blocks
+  // (0, 1) and (2, 3) that complete the half chunks beside the diagonal, dealt to
+  // the waves by diagonals, so that a lane's decay factors stay in registers.  Row
+  // i of P holds the keys of a half chunk in the order of Tile::col8.
+  constexpr int NR = STATE ? 1 : (12 + NW - 1) / NW;
+  float fac[NR][4];
+  unsigned ra[NR], rb[NR];
+  int at[NR];
+  if constexpr (!STATE) {
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const int b = n * NW + wave;
+      // diagonals 0 (4 blocks), 1 (3), 3 (1), 2 (2), then the zeros
+      const int d = b < 4 ? 0 : b < 7 ? 1 : b < 8 ? 3 : 2;
+      const int ib = b < 4 ? b : b < 7 ? b - 3 : b < 8 ? 3 : b < 10 ? b - 6 : (b - 10) * 2;
+      const int jb = b < 10 ? ib - d : ib + 1;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int lag = 16 * d + lr - 4 * lg - r;
+        fac[n][r] = lag >= 0 ? a.s_intra * powg(lg2, lag) : 0.f;
+      }
+      ra[n] = TL::row_base(lds[0][0], (ib & 3) * 16 + lr, lane);
+      rb[n] = TL::row_base(lds[0][1], (jb & 3) * 16 + lr, lane);
+      at[n] = TP::off((ib & 3) * 16 + lr, ((jb >> 1) & 1) * 32 + 8 * lg + 4 * (jb & 1));
+    }
+  }
+  const ColBase<T> bcol = TL::col_base(lds[0][1 - FIRST], lane);
+  ColBase<T> ccol = TL::col_base(lds[0][2 - FIRST], lane);  // this wave's columns
+  for (auto& x : ccol.a) x ^= wave * 16 * (int)sizeof(T);
+  const unsigned half = half_base<T, DH>(lds[0][0], lr, lane);
+  const unsigned prow = TP::row_base(P, lr, lane);
+  constexpr unsigned BUF = (3 - FIRST) * kC * DH * sizeof(T);
+#pragma unroll
+  for (int i = 0; i < NB - 1; ++i)
+    if (i < nc) issue(i, i);
 #pragma unroll
   for (int t = 0; t < NT; ++t) settle(S[t]);
-  if (NB == 2) vm_wait<0>();
+  constexpr int AHEAD = NB > 2 ? (NB - 2) * (3 - FIRST) * NI : 0;  // loads behind the next chunk's
+  if (NB - 1 <= nc) vm_wait<AHEAD>();
+  else vm_wait<0>();
+  int buf = 0, next = NB - 1;
   for (int c = 0; c < nc; ++c) {
     wg_barrier();  // this chunk's tiles are there; every wave is done with the last chunk
-    if (NB == 2) {
-      if (c + 1 < nc) issue(c + 1);
+    if (NB > 1) {
+      if (c + NB - 1 < nc) issue(c + NB - 1, next);
     } else {
-      issue(c);
+      issue(c, 0);
       vm_wait<0>();
       wg_barrier();
     }
-    const T* At = lds[NB == 2 ? c & 1 : 0][0];
-    const T* Bt = lds[NB == 2 ? c & 1 : 0][1 - FIRST];
-    const T* Ct = lds[NB == 2 ? c & 1 : 0][2 - FIRST];
+    const unsigned ba = buf * BUF;
     const int len = min(kC, sg.len - c * kC);
     f32x4 oa[4];
     F cf[2];
     if constexpr (!STATE) {
-      // scores of 16 x 16 blocks (ib, jb), jb <= ib, and the zero blocks beside
-      // the diagonal; row i of P holds the keys of a half chunk in the order of
-      // Tile::col8
-#pragma unroll 1
-      for (int blk = wave; blk < 12; blk += NW) {
-        // blocks 0..9: the triangle by rows; 10, 11: (0, 1) and (2, 3)
-        const int ib = blk < 10 ? (blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0) : (blk - 10) * 2;
-        const int jb = blk < 10 ? blk - ib * (ib + 1) / 2 : ib + 1;
+      each<NR>([&](auto n) __attribute__((always_inline)) {
+        if (n * NW + wave >= 12) return;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
-        if (blk < 10) {
-          const unsigned ra = TL::row_base(At, ib * 16 + lr, lane);
-          const unsigned rb = TL::row_base(Bt, jb * 16 + lr, lane);
+        if (n * NW + wave < 10) {
           RowRaw<T> br[KS], ar[KS];
           each<KS>([&](auto ds) {
-            br[ds] = TL::template row_at<ds, 0>(rb);
-            ar[ds] = TL::template row_at<ds, 0>(ra);
+            br[ds] = TL::template row_at<ds, 0>(rb[n] + ba);
+            ar[ds] = TL::template row_at<ds, 0>(ra[n] + ba);
           });
           lds_tr_wait();
 #pragma unroll
@@ -274,19 +320,15 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
             const F bf = TL::take_row(br[ds], lane);
             s = mma16(bf, TL::take_row(ar[ds], lane), s);
           }
-        }
-        const int i = ib * 16 + lr;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int j = jb * 16 + lg * 4 + r;
-          s[r] = blk < 10 && j <= i && j < len ? s[r] * a.s_intra * powg(lg2, i - j) : 0.f;
+          for (int r = 0; r < 4; ++r) s[r] = fac[n][r] == 0.f ? 0.f : s[r] * fac[n][r];
         }
-        store4(P + TP::off(i, (jb >> 1) * 32 + 8 * lg + 4 * (jb & 1)), s[0], s[1], s[2], s[3]);
-      }
+        store4(P + at[n], s[0], s[1], s[2], s[3]);
+      });
       // the state's term, while the scores arrive
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib) oa[ib] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const unsigned ha = half_base<T, DH>(At, lr, lane);
+      const unsigned ha = half + ba;
       each<KS>([&](auto ks) __attribute__((always_inline)) {
         const F sf = frag_from<T>(S[2 * ks], DH >= 32 ? S[2 * ks + (DH >= 32)] : f32x4{});
         HalfRaw<T> qr[4];
@@ -301,7 +343,7 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
       wg_barrier();
     }
     ColRaw<T> cr[2];
-    own_cols(cr, Ct);
+    each<2>([&](auto us) { cr[us] = TL::template col_at<0, us * 32, us * 32 + 16>(ccol, ba); });
     lds_tr_wait();
 #pragma unroll
     for (int us = 0; us < 2; ++us) cf[us] = take(cr[us]);
@@ -309,11 +351,10 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
       // A value that is not finite must not reach the rows before it through
       // 0 * inf: such columns are summed row by row.
       if (__ballot((nonfinite_bits(cf[0]) | nonfinite_bits(cf[1])) != 0) == 0) {
-        const unsigned pa = TP::row_base(P, lr, lane);
         each<4>([&](auto ib) __attribute__((always_inline)) {
           constexpr int NU = ib / 2 + 1;
           RowRaw<T> pr[NU];
-          each<NU>([&](auto us) { pr[us] = TP::template row_at<us, ib * 16>(pa); });
+          each<NU>([&](auto us) { pr[us] = TP::template row_at<us, ib * 16>(prow); });
           lds_tr_wait();
 #pragma unroll
           for (int us = 0; us < NU; ++us) oa[ib] = mma16(cf[us], take(pr[us]), oa[ib]);
@@ -326,7 +367,7 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
           for (int j = 0; j <= min(i, len - 1); ++j) {
             const int pos = (j & 32) + 8 * ((j >> 2) & 3) + ((j >> 4) & 1) * 4 + (j & 3);
             const float p = to_f32(P[TP::off(i, pos)]);
-            const f32x4 vv = load4f(Ct + TL::off(j, wave * 16 + lg * 4));
+            const f32x4 vv = load4f(lds[buf][2 - FIRST] + TL::off(j, wave * 16 + lg * 4));
 #pragma unroll
             for (int e = 0; e < 4; ++e) oa[ib][e] = fmaf(p, vv[e], oa[ib][e]);
           }
@@ -342,9 +383,12 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t) S[t] *= g;
-      add_outer<T, DH>(S, Bt, cf, w, lane);
+      add_outer<T, DH, STATE ? 2 : DH / 16>(S, bcol, ba, cf, w, a.fine);
     }
-    if (NB == 2) vm_wait<0>();  // the next chunk's tiles, before the stores
+    if (NB > 1) {  // the next chunk's tiles, before the stores
+      if (c + NB - 1 < nc) vm_wait<AHEAD>();
+      else vm_wait<0>();
+    }
     if constexpr (!STATE) {
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib) {
@@ -355,6 +399,8 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
                  oa[ib][0], oa[ib][1], oa[ib][2], oa[ib][3]);
       }
     }
+    buf = buf + 1 == NB ? 0 : buf + 1;
+    next = next + 1 == NB ? 0 : next + 1;
   }
   if (STATE) store_state<NT>(S, REV ? bs : bs + dd, DH, 1, col, lg);
   else if (a.s_out && (REV ? sg.t0 == 0 : sg.last))
@@ -384,12 +430,23 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(const int* __restrict__ c
     f32x4 u = {0.f, 0.f, 0.f, 0.f};
     if (s_in) u = *(const f32x4*)(s_in + ((int64_t)seq * H + h) * dd + e);
     if (given) *(f32x4*)(given + ((int64_t)(begin / seg + 1) * H + h) * dd + e) = u;
-    for (int i = 1; i < ns; ++i) {
-      const int k = REV ? ns - i : i;  // boundary; the segment just passed
-      const int len = REV ? min(seg, n - k * seg) : seg;
-      float* p = seg_state + ((int64_t)(begin / seg + k) * H + h) * dd + e;
-      u = u * powg(lg2, len) + *(const f32x4*)p;
-      *(f32x4*)p = u;
+    // boundary k: n - (the rows behind it), in reverse; eight sums at a time
+    float* p0 = seg_state + ((int64_t)(begin / seg) * H + h) * dd + e;
+    const int64_t step = (int64_t)H * dd;
+    const float gs = powg(lg2, seg);
+    for (int i = 1; i < ns; i += 8) {
+      f32x4 own[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        if (i + x < ns) own[x] = *(const f32x4*)(p0 + (REV ? ns - i - x : i + x) * step);
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        if (i + x < ns) {
+          const int k = REV ? ns - i - x : i + x;
+          // the segment just passed: whole, but for the last of the sequence
+          u = u * (REV && k == ns - 1 ? powg(lg2, n - k * seg) : gs) + own[x];
+          *(f32x4*)(p0 + k * step) = u;
+        }
     }
   }
 }
@@ -514,12 +571,12 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) W[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     each([&](int i) { return a.scale * (float)(i + 1) * powg(lg2, i); });
-    add_outer<T, DH>(W, lds[0], df, w, lane);
+    add_outer<T, DH>(W, TL::col_base(lds[0], lane), 0, df, w, true);
     inner(S);
 #pragma unroll
     for (int t = 0; t < NT; ++t) W[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     each([&](int i) { return a.scale * powg(lg2, i + 1); });
-    add_outer<T, DH>(W, lds[0], df, w, lane);
+    add_outer<T, DH>(W, TL::col_base(lds[0], lane), 0, df, w, true);
     inner(D);
     const float g = powg(lg2, len), g1 = (float)len * powg(lg2, len - 1);
 #pragma unroll
@@ -528,9 +585,9 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
       S[t] *= g;
     }
     each([&](int j) { return j < len - 1 ? (float)(len - 1 - j) * powg(lg2, len - 2 - j) : 0.f; });
-    add_outer<T, DH>(D, lds[1], vf, w, lane);
+    add_outer<T, DH>(D, TL::col_base(lds[1], lane), 0, vf, w, true);
     each([&](int j) { return powg(lg2, len - 1 - j); });
-    add_outer<T, DH>(S, lds[1], vf, w, lane);
+    add_outer<T, DH>(S, TL::col_base(lds[1], lane), 0, vf, w, true);
   }
   const float* R = !sg.last ? a.seg_r + bd + dd : a.ds_out ? a.ds_out + sq : nullptr;
   if (R) {
@@ -646,12 +703,20 @@ hipError_t lin_step(DType dt, int dh, const LinStep& a, hipStream_t s) {
   BY_TYPE_AND_WIDTH(step_t, dt, dh, a, s);
 }
 
-// Rows of a segment: about 512 workgroups over all heads, at least 256 rows (a
-// boundary's state, written twice and read twice, costs the traffic of a few
-// chunks).
-int lin_segment_rows(int total, int H) {
-  const int64_t want = ((int64_t)total * H / 512 + kC - 1) / kC * kC;
-  return (int)(want < 256 ? 256 : want);
+// Rows of a segment: such that the workgroups, at most total / seg + nseq of a
+// head, are one round of those that the chip holds at once (two of four waves to
+// a CU at 64 columns), or, with many sequences, a quarter of it more than these.
+// Two rounds of half the rows ran the second one with a third of the chip (131072
+// rows in 3 sequences, 16 heads of 64: the sums of 1056 segments 138 us, of 528
+// 113 us).  At least 256 rows: a boundary's state, written twice and read twice,
+// costs the traffic of a few chunks.
+int lin_segment_rows(int total, int nseq, int H, int dh) {
+  const int round = 32768 / dh / H;  // segments of a head
+  int n = round - nseq;
+  if (n < round / 4) n = round / 4;
+  if (n < 1) n = 1;
+  const int64_t want = ((int64_t)total + n - 1) / n;
+  return (int)(want < 256 ? 256 : (want + kC - 1) / kC * kC);
 }
 
 }  // namespace bcmt

@@ -138,7 +138,7 @@ struct LinPlan {
   bool cut;  // whether a sequence can have more than one segment
   size_t fwd, rev, given, part, fwd_bytes, bwd_bytes;
   explicit LinPlan(const bcmt_linattn_config& c) {
-    seg = lin_segment_rows(c.total, c.H);
+    seg = lin_segment_rows(c.total, c.nseq, c.H, c.dh);
     cut = seg < c.total;
     if (!cut) seg = (c.total + 63) / 64 * 64;
     nslot = c.total / seg + c.nseq;
@@ -385,6 +385,7 @@ int bcmt_linattn_forward(const bcmt_linattn_config* cfg, const void* q, const vo
   a.seg = pl.seg;
   a.s_intra = a.s_inter = c.scale;
   a.s_upd = 1.f;
+  a.fine = true;
   const DType dt = dtype_of(c.dtype);
   const hipStream_t s = (hipStream_t)stream;
   if (pl.cut) {
@@ -446,6 +447,7 @@ int bcmt_linattn_backward(const bcmt_linattn_config* cfg, const void* q, const v
   a.nseq = c.nseq;
   a.H = c.H;
   a.seg = pl.seg;
+  a.fine = true;  // (the same bits whatever outputs are wanted)
   auto rows = [&](const void* x, int64_t lx, const void* y, int64_t ly, const void* z, int64_t lz,
                   void* out, int64_t lo) {
     a.a = x;
@@ -476,6 +478,7 @@ int bcmt_linattn_backward(const bcmt_linattn_config* cfg, const void* q, const v
   // dq: rows dO, v, k in order, the state transposed.
   rows(dO, ldo, v, ldv, k, ldk, dq, ldq);
   a.given = nullptr;
+  a.fine = false;
   a.s_in = S_in;
   a.seg_state = seg_s;
   a.sr = 1;
@@ -520,6 +523,7 @@ int bcmt_linattn_backward(const bcmt_linattn_config* cfg, const void* q, const v
   rows(k, ldk, q, ldq, dO, ldo, dv, ldv);
   a.s_out = dS_in;
   a.given = given;
+  a.fine = true;
   a.sr = c.dh;
   a.sc = 1;
   return lin_pass(dt, c.dh, a, true, false, s) == hipSuccess ? BCMT_OK : BCMT_ERR_HIP;

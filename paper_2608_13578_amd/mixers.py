@@ -9,6 +9,8 @@ its calls must be ordered (one stream, or streams that wait for each other),
 and a captured graph replays in that workspace.
 """
 
+import ctypes
+
 import torch
 
 from . import bcmt as abi
@@ -24,18 +26,24 @@ class _Mixer:
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device(self.device.type, torch.cuda.current_device())
+        self._index = self.device.index
         self._torch_dtype = TORCH_DTYPE[dtype]
+        self._ref = ctypes.byref(cfg)
+        self._lib = abi.lib()
 
     def _scratch(self, n):
         return torch.empty(max(256, n), dtype=torch.uint8, device=self.device)
 
     def _rows(self, name, t, rows, width, ld):
-        """A tensor of `rows` rows of `width` elements (in any shape that
-        flattens to it), `ld` elements apart (0: dense)."""
-        if not isinstance(t, torch.Tensor) or t.dtype != self._torch_dtype or t.device != self.device:
+        """The address of a tensor of `rows` rows of `width` elements (in any
+        shape that flattens to it), `ld` elements apart (0: dense)."""
+        if not isinstance(t, torch.Tensor) or t.dtype != self._torch_dtype or \
+                t.get_device() != self._index:
             raise ValueError(f"{name}: a {self._torch_dtype} tensor on {self.device} is wanted")
         if t.dim() < 2 or t.shape[0] != rows or t.numel() != rows * width:
             raise ValueError(f"{name}: {rows} rows of {width} elements are wanted, got {tuple(t.shape)}")
+        if ld in (0, width) and t.is_contiguous():
+            return t.data_ptr()
         if rows > 1 and t.stride(0) != (ld or width):
             raise ValueError(f"{name}: row stride {ld or width} is wanted, got {t.stride(0)}")
         n = 1
@@ -43,20 +51,31 @@ class _Mixer:
             if t.shape[d] > 1 and t.stride(d) != n:
                 raise ValueError(f"{name}: the elements of a row must be contiguous")
             n *= t.shape[d]
+        return t.data_ptr()
 
     def _array(self, name, t, shape, dtype, optional=False):
+        """The address of a contiguous tensor of this shape and type."""
         if t is None and optional:
-            return
-        if (not isinstance(t, torch.Tensor) or t.dtype != dtype or tuple(t.shape) != tuple(shape)
-                or not t.is_contiguous() or t.device != self.device):
+            return None
+        if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape
+                or t.get_device() != self._index or not t.is_contiguous()):
             raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on "
                              f"{self.device} is wanted")
+        return t.data_ptr()
 
-    def _on(self, stream):
-        """The caller's stream, or the current one of this object's device."""
+    def _call(self, fn, stream, *args):
+        """Enqueues on the caller's stream, or the current one of this object's
+        device, which is made the current device for the call."""
         if stream is None:
-            return torch.cuda.current_stream(self.device)
-        return stream
+            stream = torch.cuda.current_stream(self._index)
+        s = stream if isinstance(stream, int) else stream.cuda_stream
+        if torch.cuda.current_device() == self._index:
+            st = fn(self._ref, *args, s)
+        else:
+            with torch.cuda.device(self._index):
+                st = fn(self._ref, *args, s)
+        if st != abi.BCMT_OK:
+            raise abi.BcmtError(st, fn.__name__)
 
 
 class PackedAttention(_Mixer):
@@ -68,42 +87,37 @@ class PackedAttention(_Mixer):
         self._setup(abi.make_attn_config(total, nseq, H, Hkv, dh, dtype, scale, ldq, ldk, ldv, ldo),
                     abi.bcmt_attn_validate, dtype, device)
         self.ws = None
+        self._total, self._nseq, self._H = total, nseq, H
+        self._wq, self._wk = H * dh, Hkv * dh
+        self._ld = ldq, ldk, ldv, ldo
 
-    def _check(self, q, k, v, cu, o):
-        c = self.cfg
-        self._rows("q", q, c.total, c.H * c.dh, c.ldq)
-        self._rows("k", k, c.total, c.Hkv * c.dh, c.ldk)
-        self._rows("v", v, c.total, c.Hkv * c.dh, c.ldv)
-        self._rows("o", o, c.total, c.H * c.dh, c.ldo)
-        self._array("cu", cu, (c.nseq + 1,), torch.int32)
+    def _inputs(self, q, k, v, cu):
+        n, (ldq, ldk, ldv, _) = self._total, self._ld
+        return (self._rows("q", q, n, self._wq, ldq), self._rows("k", k, n, self._wk, ldk),
+                self._rows("v", v, n, self._wk, ldv),
+                self._array("cu", cu, (self._nseq + 1,), torch.int32))
 
     def new_output(self):
-        c = self.cfg
-        return torch.empty((c.total, c.ldo or c.H * c.dh), dtype=self._torch_dtype,
-                           device=self.device)[:, :c.H * c.dh]
+        return torch.empty((self._total, self._ld[3] or self._wq), dtype=self._torch_dtype,
+                           device=self.device)[:, :self._wq]
 
     def new_lse(self):
-        return torch.empty((self.cfg.H, self.cfg.total), dtype=torch.float32, device=self.device)
+        return torch.empty((self._H, self._total), dtype=torch.float32, device=self.device)
 
     def forward(self, q, k, v, cu, o, lse=None, stream=None):
-        self._check(q, k, v, cu, o)
-        self._array("lse", lse, (self.cfg.H, self.cfg.total), torch.float32, optional=True)
-        with torch.cuda.device(self.device):
-            abi.bcmt_attn_forward(self.cfg, q, k, v, cu, o, lse, stream=self._on(stream))
+        self._call(self._lib.bcmt_attn_forward, stream, *self._inputs(q, k, v, cu),
+                   self._rows("o", o, self._total, self._wq, self._ld[3]),
+                   self._array("lse", lse, (self._H, self._total), torch.float32, True))
 
     def backward(self, q, k, v, cu, o, lse, dO, dq, dk, dv, stream=None):
-        c = self.cfg
-        self._check(q, k, v, cu, o)
-        self._array("lse", lse, (c.H, c.total), torch.float32)
-        self._rows("dO", dO, c.total, c.H * c.dh, c.ldo)
-        self._rows("dq", dq, c.total, c.H * c.dh, c.ldq)
-        self._rows("dk", dk, c.total, c.Hkv * c.dh, c.ldk)
-        self._rows("dv", dv, c.total, c.Hkv * c.dh, c.ldv)
+        n, wq, wk, (ldq, ldk, ldv, ldo) = self._total, self._wq, self._wk, self._ld
+        args = (*self._inputs(q, k, v, cu), self._rows("o", o, n, wq, ldo),
+                self._array("lse", lse, (self._H, n), torch.float32),
+                self._rows("dO", dO, n, wq, ldo), self._rows("dq", dq, n, wq, ldq),
+                self._rows("dk", dk, n, wk, ldk), self._rows("dv", dv, n, wk, ldv))
         if self.ws is None:
-            self.ws = self._scratch(abi.bcmt_attn_workspace_bytes(c))
-        with torch.cuda.device(self.device):
-            abi.bcmt_attn_backward(c, q, k, v, cu, o, lse, dO, dq, dk, dv, self.ws,
-                                   stream=self._on(stream))
+            self.ws = self._scratch(abi.bcmt_attn_workspace_bytes(self.cfg))
+        self._call(self._lib.bcmt_attn_backward, stream, *args, self.ws.data_ptr(), self.ws.numel())
 
 
 class AttentionDecoder(_Mixer):
@@ -116,37 +130,34 @@ class AttentionDecoder(_Mixer):
                                                 ldv, ldo, cs, ct, ch),
                     abi.bcmt_attn_decode_validate, dtype, device)
         self.ws = self._scratch(abi.bcmt_attn_decode_workspace_bytes(self.cfg))
+        self._B, self._wq, self._wk = B, H * dh, Hkv * dh
+        self._ld = ldq, ldk, ldv, ldo
+        self._shape = (slots, cap, Hkv, dh)
+        self._strides = (cs or cap * Hkv * dh, ct or Hkv * dh, ch or dh, 1)
 
     def new_cache(self):
         """A dense cache for keys or values."""
-        c = self.cfg
-        return torch.zeros((c.slots, c.cap, c.Hkv, c.dh), dtype=self._torch_dtype,
-                           device=self.device)
+        return torch.zeros(self._shape, dtype=self._torch_dtype, device=self.device)
 
     def _cache(self, name, t):
-        c = self.cfg
-        shape = (c.slots, c.cap, c.Hkv, c.dh)
-        if not isinstance(t, torch.Tensor) or t.dtype != self._torch_dtype or t.device != self.device:
+        if not isinstance(t, torch.Tensor) or t.dtype != self._torch_dtype or \
+                t.get_device() != self._index:
             raise ValueError(f"{name}: a {self._torch_dtype} tensor on {self.device} is wanted")
-        want = (c.cs or c.cap * c.Hkv * c.dh, c.ct or c.Hkv * c.dh, c.ch or c.dh, 1)
-        if tuple(t.shape) != shape or any(n > 1 and s != w for n, s, w in
-                                          zip(shape, t.stride(), want)):
+        shape, want = self._shape, self._strides
+        if t.shape != shape or (t.stride() != want and any(
+                n > 1 and s != w for n, s, w in zip(shape, t.stride(), want))):
             raise ValueError(f"{name}: shape {shape} with strides {want} is wanted, got "
                              f"{tuple(t.shape)} with {t.stride()}")
+        return t.data_ptr()
 
     def step(self, q, k, v, slot, length, kcache, vcache, o, stream=None):
-        c = self.cfg
-        self._rows("q", q, c.B, c.H * c.dh, c.ldq)
-        self._rows("k", k, c.B, c.Hkv * c.dh, c.ldk)
-        self._rows("v", v, c.B, c.Hkv * c.dh, c.ldv)
-        self._rows("o", o, c.B, c.H * c.dh, c.ldo)
-        self._array("slot", slot, (c.B,), torch.int32, optional=True)
-        self._array("length", length, (c.B,), torch.int32)
-        self._cache("kcache", kcache)
-        self._cache("vcache", vcache)
-        with torch.cuda.device(self.device):
-            abi.bcmt_attn_decode(c, q, k, v, slot, length, kcache, vcache, o, self.ws,
-                                 stream=self._on(stream))
+        n, wq, wk, (ldq, ldk, ldv, ldo) = self._B, self._wq, self._wk, self._ld
+        self._call(self._lib.bcmt_attn_decode, stream, self._rows("q", q, n, wq, ldq),
+                   self._rows("k", k, n, wk, ldk), self._rows("v", v, n, wk, ldv),
+                   self._array("slot", slot, (n,), torch.int32, True),
+                   self._array("length", length, (n,), torch.int32),
+                   self._cache("kcache", kcache), self._cache("vcache", vcache),
+                   self._rows("o", o, n, wq, ldo), self.ws.data_ptr(), self.ws.numel())
 
 
 class LinearAttention(_Mixer):
@@ -159,52 +170,42 @@ class LinearAttention(_Mixer):
                     abi.bcmt_linattn_validate, dtype, device)
         self.ws = self._scratch(abi.bcmt_linattn_workspace_bytes(self.cfg, abi.BCMT_PASS_FORWARD))
         self.ws_bwd = None
+        self._total, self._nseq, self._H, self._w = total, nseq, H, H * dh
+        self._ld = ldq, ldk, ldv, ldo
+        self._shape = (nseq, H, dh, dh)
 
     def new_state(self):
         """Zero states: empty histories."""
-        c = self.cfg
-        return torch.zeros((c.nseq, c.H, c.dh, c.dh), dtype=torch.float32, device=self.device)
+        return torch.zeros(self._shape, dtype=torch.float32, device=self.device)
 
-    def _check(self, q, k, v, gamma, cu):
-        c = self.cfg
-        w = c.H * c.dh
-        self._rows("q", q, c.total, w, c.ldq)
-        self._rows("k", k, c.total, w, c.ldk)
-        self._rows("v", v, c.total, w, c.ldv)
-        self._array("gamma", gamma, (c.H,), torch.float32)
-        self._array("cu", cu, (c.nseq + 1,), torch.int32)
+    def _inputs(self, q, k, v, gamma, cu):
+        n, w, (ldq, ldk, ldv, _) = self._total, self._w, self._ld
+        return (self._rows("q", q, n, w, ldq), self._rows("k", k, n, w, ldk),
+                self._rows("v", v, n, w, ldv),
+                self._array("gamma", gamma, (self._H,), torch.float32),
+                self._array("cu", cu, (self._nseq + 1,), torch.int32))
 
     def _state(self, name, t):
-        c = self.cfg
-        self._array(name, t, (c.nseq, c.H, c.dh, c.dh), torch.float32, optional=True)
+        return self._array(name, t, self._shape, torch.float32, True)
 
     def forward(self, q, k, v, gamma, cu, o, S_in=None, S_out=None, stream=None):
-        c = self.cfg
-        self._check(q, k, v, gamma, cu)
-        self._rows("o", o, c.total, c.H * c.dh, c.ldo)
-        self._state("S_in", S_in)
-        self._state("S_out", S_out)
-        with torch.cuda.device(self.device):
-            abi.bcmt_linattn_forward(c, q, k, v, gamma, cu, S_in, o, S_out, self.ws,
-                                     stream=self._on(stream))
+        self._call(self._lib.bcmt_linattn_forward, stream, *self._inputs(q, k, v, gamma, cu),
+                   self._state("S_in", S_in), self._rows("o", o, self._total, self._w, self._ld[3]),
+                   self._state("S_out", S_out), self.ws.data_ptr(), self.ws.numel())
 
     def backward(self, q, k, v, gamma, cu, dO, dq, dk, dv, S_in=None, dS_out=None, dS_in=None,
                  dgamma=None, stream=None):
-        c = self.cfg
-        w = c.H * c.dh
-        self._check(q, k, v, gamma, cu)
-        self._rows("dO", dO, c.total, w, c.ldo)
-        self._rows("dq", dq, c.total, w, c.ldq)
-        self._rows("dk", dk, c.total, w, c.ldk)
-        self._rows("dv", dv, c.total, w, c.ldv)
-        for name, t in (("S_in", S_in), ("dS_out", dS_out), ("dS_in", dS_in)):
-            self._state(name, t)
-        self._array("dgamma", dgamma, (c.H,), torch.float32, optional=True)
+        n, w, (ldq, ldk, ldv, ldo) = self._total, self._w, self._ld
+        args = (*self._inputs(q, k, v, gamma, cu), self._state("S_in", S_in),
+                self._rows("dO", dO, n, w, ldo), self._state("dS_out", dS_out),
+                self._rows("dq", dq, n, w, ldq), self._rows("dk", dk, n, w, ldk),
+                self._rows("dv", dv, n, w, ldv), self._state("dS_in", dS_in),
+                self._array("dgamma", dgamma, (self._H,), torch.float32, True))
         if self.ws_bwd is None:
-            self.ws_bwd = self._scratch(abi.bcmt_linattn_workspace_bytes(c, abi.BCMT_PASS_BACKWARD))
-        with torch.cuda.device(self.device):
-            abi.bcmt_linattn_backward(c, q, k, v, gamma, cu, S_in, dO, dS_out, dq, dk, dv, dS_in,
-                                      dgamma, self.ws_bwd, stream=self._on(stream))
+            self.ws_bwd = self._scratch(abi.bcmt_linattn_workspace_bytes(self.cfg,
+                                                                         abi.BCMT_PASS_BACKWARD))
+        self._call(self._lib.bcmt_linattn_backward, stream, *args, self.ws_bwd.data_ptr(),
+                   self.ws_bwd.numel())
 
 
 class LinearAttentionDecoder(_Mixer):
@@ -215,19 +216,19 @@ class LinearAttentionDecoder(_Mixer):
                  device="cuda"):
         self._setup(abi.make_linattn_step_config(B, slots, H, dh, dtype, scale, ldq, ldk, ldv, ldo),
                     abi.bcmt_linattn_step_validate, dtype, device)
+        self._B, self._H, self._w = B, H, H * dh
+        self._ld = ldq, ldk, ldv, ldo
+        self._shape = (slots, H, dh, dh)
 
     def new_state(self):
-        c = self.cfg
-        return torch.zeros((c.slots, c.H, c.dh, c.dh), dtype=torch.float32, device=self.device)
+        return torch.zeros(self._shape, dtype=torch.float32, device=self.device)
 
     def step(self, q, k, v, gamma, slot, S_in, S_out, o, stream=None):
-        c = self.cfg
-        w = c.H * c.dh
-        for name, t, ld in (("q", q, c.ldq), ("k", k, c.ldk), ("v", v, c.ldv), ("o", o, c.ldo)):
-            self._rows(name, t, c.B, w, ld)
-        self._array("gamma", gamma, (c.H,), torch.float32)
-        self._array("slot", slot, (c.B,), torch.int32, optional=True)
-        self._array("S_in", S_in, (c.slots, c.H, c.dh, c.dh), torch.float32)
-        self._array("S_out", S_out, (c.slots, c.H, c.dh, c.dh), torch.float32)
-        with torch.cuda.device(self.device):
-            abi.bcmt_linattn_step(c, q, k, v, gamma, slot, S_in, S_out, o, stream=self._on(stream))
+        n, w, (ldq, ldk, ldv, ldo) = self._B, self._w, self._ld
+        self._call(self._lib.bcmt_linattn_step, stream, self._rows("q", q, n, w, ldq),
+                   self._rows("k", k, n, w, ldk), self._rows("v", v, n, w, ldv),
+                   self._array("gamma", gamma, (self._H,), torch.float32),
+                   self._array("slot", slot, (n,), torch.int32, True),
+                   self._array("S_in", S_in, self._shape, torch.float32),
+                   self._array("S_out", S_out, self._shape, torch.float32),
+                   self._rows("o", o, n, w, ldo))
