@@ -429,8 +429,30 @@ struct LinPass {
   int64_t lda, ldb, ldc, ldo;
   float s_intra, s_inter, s_upd;  // factors of the scores, of the state's term, of its update
   bool fine;  // the state can be an output: sums of 24 bits, not 16
+  // the joined dq pass (in order): also scale sum g^(i+1) q_i a_i^T of every segment but the
+  // first -> sum_state, laid out as seg_state
+  const void* q;
+  int64_t ldq;
+  float* sum_state;
+  float s_sum;
 };
-// state: only the segments' own sums -> seg_state (rows b, columns c).
+// dk and dv in one reverse pass (seg_state: the gradients of the states at the
+// boundaries; given: see above).
+struct LinPair {
+  const void *k, *v, *q, *dout;
+  void *dk, *dv;  // strides of k, v
+  const int* cu;
+  const float *gamma, *ds_out;
+  float *ds_in, *seg_state, *given;
+  int total, nseq, H, seg;
+  int64_t ldk, ldv, ldq, ldo;
+  float scale;
+};
+hipError_t lin_dkdv(int dh, const LinPair& a, hipStream_t s);
+// Whether the gradient runs so: dq with the sums of R, then dk and dv together.
+bool lin_joined_backward(DType dt, int dh);
+// state: only the segments' own sums -> seg_state (rows b, columns c).  In reverse (rev) only
+// where the gradient's passes run apart (lin_joined_backward).
 hipError_t lin_pass(DType dt, int dh, const LinPass& a, bool rev, bool state, hipStream_t s);
 // Those sums -> the states at the boundaries between segments (s_in unswapped).
 hipError_t lin_scan(int dh, const LinPass& a, bool rev, hipStream_t s);

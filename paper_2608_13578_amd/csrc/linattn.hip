@@ -179,18 +179,22 @@ constexpr int lin_buffers(bool state) {
 }
 
 // ------------------------------------------------------------------ the operator
-// REV: rows in reverse.  STATE: only the segment's own sum of states.
+// REV: rows in reverse.  STATE: only the segment's own sum of states.  SUM: the
+// gradient's dq pass, which also leaves the segment's own sum of R, scale sum_i
+// g^(i+1) q_i do_i^T, for the reverse pass (its rows a are do; q is a fourth tile):
+// the local index runs forward, so the sum needs no decay, only falling weights.
 
-template <typename T, int DH, bool REV, bool STATE>
-__global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
+template <typename T, int DH, bool REV, bool STATE, bool SUM>
+__global__ __launch_bounds__(DH * 4, sizeof(T) == 2 ? 2 : 1) void lin_kernel(LinPass a) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
   typedef Tile<T, kC> TP;
   constexpr int NW = DH / 16, NT = DH / 16, KS = DH >= 32 ? DH / 32 : 1;
   constexpr int FIRST = STATE ? 1 : 0;  // tiles a, b, c: the sum needs b and c
-  constexpr int NB = lin_buffers<T, DH>(STATE);
+  constexpr int TILES = SUM ? 4 : 3 - FIRST;
+  constexpr int NB = SUM ? 2 : lin_buffers<T, DH>(STATE);
   constexpr int NI = TL::NCH / NW;  // loads of a tile by each wave
-  __shared__ __attribute__((aligned(1024))) T lds[NB][3 - FIRST][kC * DH];
+  __shared__ __attribute__((aligned(1024))) T lds[NB][TILES][kC * DH];
   __shared__ __attribute__((aligned(1024))) T P[STATE ? 16 : kC * kC];
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
@@ -223,6 +227,7 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
   const T* A = STATE ? nullptr : (const T*)a.a + r0 * a.lda + h * DH;
   const T* B = (const T*)a.b + r0 * a.ldb + h * DH;
   const T* Cc = (const T*)a.c + r0 * a.ldc + h * DH;
+  const T* Q = SUM ? (const T*)a.q + r0 * a.ldq + h * DH : nullptr;
   auto issue = [=](int c, int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -230,6 +235,7 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
       if (!STATE) TL::issue(A, la, c * kC, sg.len - 1, lds[buf][0], ti, lane);
       TL::issue(B, lb, c * kC, sg.len - 1, lds[buf][1 - FIRST], ti, lane);
       TL::issue(Cc, lc, c * kC, sg.len - 1, lds[buf][2 - FIRST], ti, lane);
+      if (SUM) TL::issue(Q, a.ldq, c * kC, sg.len - 1, lds[buf][TILES - 1], ti, lane);
     }
   };
   // g^(64 - 1 - j) (forward) or g^(64 - j) (reverse) for the rows this lane
@@ -281,13 +287,28 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
   for (auto& x : ccol.a) x ^= wave * 16 * (int)sizeof(T);
   const unsigned half = half_base<T, DH>(lds[0][0], lr, lane);
   const unsigned prow = TP::row_base(P, lr, lane);
-  constexpr unsigned BUF = (3 - FIRST) * kC * DH * sizeof(T);
+  constexpr unsigned BUF = TILES * kC * DH * sizeof(T);
+  // SUM: q's columns, do's columns of this wave; R's part, its weights, g^(64 c)
+  const ColBase<T> qcol = TL::col_base(lds[0][TILES - 1], lane);
+  ColBase<T> dcol = TL::col_base(lds[0][0], lane);
+  for (auto& x : dcol.a) x ^= wave * 16 * (int)sizeof(T);
+  f32x4 R[SUM ? NT : 1];
+  float wr[2][8], gc = 1.f;
+  if constexpr (SUM) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) R[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int us = 0; us < 2; ++us)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        wr[us][e] = a.s_sum * powg(lg2, us * 32 + (e < 4 ? 4 * lg + e : 12 + 4 * lg + e) + 1);
+  }
 #pragma unroll
   for (int i = 0; i < NB - 1; ++i)
     if (i < nc) issue(i, i);
 #pragma unroll
   for (int t = 0; t < NT; ++t) settle(S[t]);
-  constexpr int AHEAD = NB > 2 ? (NB - 2) * (3 - FIRST) * NI : 0;  // loads behind the next chunk's
+  constexpr int AHEAD = NB > 2 ? (NB - 2) * TILES * NI : 0;  // loads behind the next chunk's
   if (NB - 1 <= nc) vm_wait<AHEAD>();
   else vm_wait<0>();
   int buf = 0, next = NB - 1;
@@ -383,7 +404,25 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t) S[t] *= g;
-      add_outer<T, DH, STATE ? 2 : DH / 16>(S, bcol, ba, cf, w, a.fine);
+      add_outer<T, DH, STATE ? 2 : SUM ? 4 : DH / 16>(S, bcol, ba, cf, w, a.fine);
+    }
+    if constexpr (SUM) {
+      if (sg.t0 > 0) {  // (the sequence's first segment has no boundary before it)
+        ColRaw<T> dr[2];
+        each<2>([&](auto us) { dr[us] = TL::template col_at<0, us * 32, us * 32 + 16>(dcol, ba); });
+        lds_tr_wait();
+        F df[2];
+        float wc[2][8];
+#pragma unroll
+        for (int us = 0; us < 2; ++us) {
+          df[us] = take(dr[us]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            wc[us][e] = us * 32 + (e < 4 ? 4 * lg + e : 12 + 4 * lg + e) < len ? wr[us][e] * gc : 0.f;
+        }
+        add_outer<T, DH, 4>(R, qcol, ba, df, wc, true);
+        gc *= gC;
+      }
     }
     if (NB > 1) {  // the next chunk's tiles, before the stores
       if (c + NB - 1 < nc) vm_wait<AHEAD>();
@@ -402,9 +441,202 @@ __global__ __launch_bounds__(DH * 4) void lin_kernel(LinPass a) {
     buf = buf + 1 == NB ? 0 : buf + 1;
     next = next + 1 == NB ? 0 : next + 1;
   }
+  if constexpr (SUM) {
+    if (sg.t0 > 0)
+      store_state<NT>(R, a.sum_state + sg.bound * dd + (int64_t)h * DH * DH, DH, 1, col, lg);
+  }
   if (STATE) store_state<NT>(S, REV ? bs : bs + dd, DH, 1, col, lg);
   else if (a.s_out && (REV ? sg.t0 == 0 : sg.last))
     store_state<NT>(S, a.s_out + sq, a.sr, a.sc, col, lg);
+}
+
+// dk and dv in one reverse pass (bf16, up to 64 columns): two roles of the operator over the same
+// four tiles,
+//   role 0: a, b, c = k, q, do -> dv, the state R [q][do];
+//   role 1: a, b, c = v, do, q -> dk, its transpose;
+// the rows are read once for both, and a chunk's two barriers are shared.  8192
+// rows, 12 heads of 64: 28 us against 20 + 20 us.  With 128 columns a pass is bound
+// by what its eight waves read from LDS and issue, not by its rows (32768 rows, 16
+// heads: 356 us against 161 + 161 us, and 243 us for dq with the sum of R against
+// 161 + 87 us), so those stay apart.
+template <int DH>
+__global__ __launch_bounds__(DH * 4, 2) void lin_dkdv_kernel(LinPair a) {
+  typedef bf16 T;
+  typedef bf16x8 F;
+  typedef Tile<T, DH> TL;
+  typedef Tile<T, kC> TP;
+  constexpr int NW = DH / 16, NT = DH / 16, KS = DH >= 32 ? DH / 32 : 1, NI = TL::NCH / NW;
+  constexpr unsigned TILE = kC * DH * sizeof(T), BUF = 4 * TILE, PB = kC * kC * sizeof(T);
+  __shared__ __attribute__((aligned(1024))) T lds[2][4][kC * DH];  // k, v, q, do
+  __shared__ __attribute__((aligned(1024))) T P[2][kC * kC];
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  const int lr = lane & 15, lg = lane >> 4;
+  const int h = blockIdx.x % a.H;
+  const LinSeg sg = lin_segment(a.cu, a.nseq, a.total, a.seg, blockIdx.x / a.H);
+  if (sg.len < 0) return;
+  const float lg2 = log2f(a.gamma[h]);
+  const int col = wave * 16 + lr;
+
+  f32x4 S[2][NT];
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) S[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int64_t dd = (int64_t)a.H * DH * DH, hs = (int64_t)h * DH * DH, sq = sg.seq * dd + hs;
+  const float* from = !sg.last              ? a.seg_state + (sg.bound + 1) * dd + hs
+                      : a.given && sg.t0 > 0 ? a.given + sg.first * dd + hs
+                      : a.ds_out            ? a.ds_out + sq
+                                            : nullptr;
+  if (from) {
+    load_state<NT>(S[0], from, DH, 1, col, lg);
+    load_state<NT>(S[1], from, 1, DH, col, lg);
+  }
+  const int nc = (sg.len + kC - 1) / kC;
+  const int64_t r0 = sg.row0 + sg.len - 1;
+  const T* K = (const T*)a.k + r0 * a.ldk + h * DH;
+  const T* V = (const T*)a.v + r0 * a.ldv + h * DH;
+  const T* Q = (const T*)a.q + r0 * a.ldq + h * DH;
+  const T* O = (const T*)a.dout + r0 * a.ldo + h * DH;
+  auto issue = [=](int c, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int ti = wave * NI + i;
+      TL::issue(K, -a.ldk, c * kC, sg.len - 1, lds[buf][0], ti, lane);
+      TL::issue(V, -a.ldv, c * kC, sg.len - 1, lds[buf][1], ti, lane);
+      TL::issue(Q, -a.ldq, c * kC, sg.len - 1, lds[buf][2], ti, lane);
+      TL::issue(O, -a.ldo, c * kC, sg.len - 1, lds[buf][3], ti, lane);
+    }
+  };
+  float w[2][8], fi[4];
+  auto weights = [&](int len) __attribute__((always_inline)) {
+#pragma unroll
+    for (int us = 0; us < 2; ++us)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int j = us * 32 + (e < 4 ? 4 * lg + e : 12 + 4 * lg + e);
+        w[us][e] = j < len ? a.scale * powg(lg2, len - j) : 0.f;
+      }
+  };
+  weights(kC);
+#pragma unroll
+  for (int ib = 0; ib < 4; ++ib) fi[ib] = powg(lg2, ib * 16 + lr);
+  const float gC = powg(lg2, kC);
+  // the blocks of the scores, as above
+  constexpr int NR = (12 + NW - 1) / NW;
+  float fac[NR][4];
+  unsigned ra[NR], rb[NR];
+  int at[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int b = n * NW + wave;
+    const int d = b < 4 ? 0 : b < 7 ? 1 : b < 8 ? 3 : 2;
+    const int ib = b < 4 ? b : b < 7 ? b - 3 : b < 8 ? 3 : b < 10 ? b - 6 : (b - 10) * 2;
+    const int jb = b < 10 ? ib - d : ib + 1;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int lag = 16 * d + lr - 4 * lg - r;
+      fac[n][r] = lag >= 0 ? a.scale * powg(lg2, lag) : 0.f;
+    }
+    ra[n] = TL::row_base(lds[0][0], (ib & 3) * 16 + lr, lane);
+    rb[n] = TL::row_base(lds[0][2], (jb & 3) * 16 + lr, lane);
+    at[n] = TP::off((ib & 3) * 16 + lr, ((jb >> 1) & 1) * 32 + 8 * lg + 4 * (jb & 1));
+  }
+  const ColBase<T> bcol = TL::col_base(lds[0][2], lane);
+  ColBase<T> ccol = TL::col_base(lds[0][2], lane);  // this wave's columns (of role 1)
+  ccol.a[0] ^= wave * 16 * (int)sizeof(T);
+  const unsigned half = half_base<T, DH>(lds[0][0], lr, lane);
+  const unsigned prow = TP::row_base(P[0], lr, lane);
+
+  if (nc > 0) issue(0, 0);
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) settle(S[p][t]);
+  vm_wait<0>();
+  for (int c = 0; c < nc; ++c) {
+    wg_barrier();  // this chunk's tiles are there; every wave is done with the last chunk
+    if (c + 1 < nc) issue(c + 1, (c + 1) & 1);
+    const int buf = c & 1, len = min(kC, sg.len - c * kC);
+    const unsigned ba = buf * BUF;
+    f32x4 oa[2][4];
+    each<2>([&](auto p) __attribute__((always_inline)) {
+      each<NR>([&](auto n) __attribute__((always_inline)) {
+        if (n * NW + wave >= 12) return;
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        if (n * NW + wave < 10) {
+          RowRaw<T> br[KS], ar[KS];
+          each<KS>([&](auto ds) {
+            br[ds] = TL::template row_at<ds, 0>(rb[n] + (ba + p * TILE));
+            ar[ds] = TL::template row_at<ds, 0>(ra[n] + (ba + p * TILE));
+          });
+          lds_tr_wait();
+#pragma unroll
+          for (int ds = 0; ds < KS; ++ds) {
+            const F bf = TL::take_row(br[ds], lane);
+            s = mma16(bf, TL::take_row(ar[ds], lane), s);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[r] = fac[n][r] == 0.f ? 0.f : s[r] * fac[n][r];
+        }
+        store4(P[p] + at[n], s[0], s[1], s[2], s[3]);
+      });
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib) oa[p][ib] = f32x4{0.f, 0.f, 0.f, 0.f};
+      each<KS>([&](auto ks) __attribute__((always_inline)) {
+        const F sf = frag_from<T>(S[p][2 * ks], DH >= 32 ? S[p][2 * ks + (DH >= 32)] : f32x4{});
+        HalfRaw<T> qr[4];
+        each<4>([&](auto ib) { qr[ib] = half_at<T, DH, ks, ib * 16>(half + (ba + p * TILE)); });
+        lds_tr_wait();
+#pragma unroll
+        for (int ib = 0; ib < 4; ++ib) oa[p][ib] = mma16(sf, take_row8p<T, DH>(qr[ib]), oa[p][ib]);
+      });
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib) oa[p][ib] *= fi[ib];
+    });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the scores are written
+    wg_barrier();
+    const bool more = c + 1 < nc || a.ds_in;
+    float g = gC;
+    if (len < kC && more) {
+      weights(len);
+      g = powg(lg2, len);
+    }
+    each<2>([&](auto p) __attribute__((always_inline)) {
+      ColRaw<T> cr[2];
+      F cf[2];
+      const unsigned ca = ba + (1 - p) * TILE;  // c is q for role 1, do for role 0
+      each<2>([&](auto us) { cr[us] = TL::template col_at<0, us * 32, us * 32 + 16>(ccol, ca); });
+      lds_tr_wait();
+#pragma unroll
+      for (int us = 0; us < 2; ++us) cf[us] = take(cr[us]);
+      each<4>([&](auto ib) __attribute__((always_inline)) {
+        constexpr int NU = ib / 2 + 1;
+        RowRaw<T> pr[NU];
+        each<NU>([&](auto us) { pr[us] = TP::template row_at<us, ib * 16>(prow + p * PB); });
+        lds_tr_wait();
+#pragma unroll
+        for (int us = 0; us < NU; ++us) oa[p][ib] = mma16(cf[us], take(pr[us]), oa[p][ib]);
+      });
+      if (more) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[p][t] *= g;
+        add_outer<T, DH, 4>(S[p], bcol, ba + p * TILE, cf, w, p == 0);
+      }
+    });
+    vm_wait<0>();  // the next chunk's tiles, before the stores
+#pragma unroll
+    for (int ib = 0; ib < 4; ++ib) {
+      const int i = ib * 16 + lr;
+      if (i < len) {
+        const int64_t r = r0 - (c * kC + i);
+        store4((T*)a.dv + r * a.ldv + h * DH + wave * 16 + lg * 4, oa[0][ib][0], oa[0][ib][1],
+               oa[0][ib][2], oa[0][ib][3]);
+        store4((T*)a.dk + r * a.ldk + h * DH + wave * 16 + lg * 4, oa[1][ib][0], oa[1][ib][1],
+               oa[1][ib][2], oa[1][ib][3]);
+      }
+    }
+  }
+  if (a.ds_in && sg.t0 == 0) store_state<NT>(S[0], a.ds_in + sq, DH, 1, col, lg);
 }
 
 // The segments' own sums -> the states at the boundaries, in place, from the
@@ -468,8 +700,9 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
   constexpr int NW = DH / 16, NT = DH / 16, KS = DH >= 32 ? DH / 32 : 1;
-  constexpr int NI = TL::NCH / NW;
-  __shared__ __attribute__((aligned(1024))) T lds[4][kC * DH];  // q, k, v, do
+  constexpr int NI = TL::NCH / NW, NB = sizeof(T) * DH > 256 ? 1 : 2;
+  __shared__ __attribute__((aligned(1024))) T ring[NB][4][kC * DH];  // q, k, v, do
+  __shared__ __attribute__((aligned(16))) float tab[2][3][kC];
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int h = blockIdx.x % a.H, slot = blockIdx.x / a.H;
@@ -499,23 +732,63 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
   const T* ds_ = (const T*)a.dout + sg.row0 * a.ldo + h * DH;
   float sum = 0.f;
   const int nc = (sg.len + kC - 1) / kC;
-  for (int c = 0; c < nc; ++c) {
-    wg_barrier();
+  auto issue = [=](int c) __attribute__((always_inline)) {
+    T(*t)[kC * DH] = ring[NB == 2 ? c & 1 : 0];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int ti = wave * NI + i;
-      TL::issue(qs, a.ldq, c * kC, sg.len - 1, lds[0], ti, lane);
-      TL::issue(ks_, a.ldk, c * kC, sg.len - 1, lds[1], ti, lane);
-      TL::issue(vs, a.ldv, c * kC, sg.len - 1, lds[2], ti, lane);
-      TL::issue(ds_, a.ldo, c * kC, sg.len - 1, lds[3], ti, lane);
+      TL::issue(qs, a.ldq, c * kC, sg.len - 1, t[0], ti, lane);
+      TL::issue(ks_, a.ldk, c * kC, sg.len - 1, t[1], ti, lane);
+      TL::issue(vs, a.ldv, c * kC, sg.len - 1, t[2], ti, lane);
+      TL::issue(ds_, a.ldo, c * kC, sg.len - 1, t[3], ti, lane);
     }
-    vm_wait<0>();
-    wg_barrier();
+  };
+  // The weights of a chunk's rows j, for a whole chunk and for the last one: g^j,
+  // g^(len-1-j) and (len-1-j) g^(len-2-j); and each lane's factors (i-j) g^(i-j-1) of
+  // the scores.  (Powers formed anew for every use took half of this kernel.)
+  if (threadIdx.x < kC) {
+    const int j = threadIdx.x;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int len = x ? sg.len - (nc - 1) * kC : kC;
+      tab[x][0][j] = j < len ? powg(lg2h, j) : 0.f;
+      tab[x][1][j] = j < len ? powg(lg2h, len - 1 - j) : 0.f;
+      tab[x][2][j] = j < len - 1 ? (float)(len - 1 - j) * powg(lg2h, len - 2 - j) : 0.f;
+    }
+  }
+  constexpr int NR = (10 + NW - 1) / NW;
+  float fac[NR][4];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int blk = n * NW + wave;
+    const int ib = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, jb = blk - ib * (ib + 1) / 2;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int lag = (ib - jb) * 16 + lr - lg * 4 - r;
+      fac[n][r] = lag > 0 ? a.scale * (float)lag * powg(lg2h, lag - 1) : 0.f;
+    }
+  }
+  const float gh = a.gamma[h], gC = powg(lg2h, kC), gC1 = powg(lg2h, kC - 1);
+  __syncthreads();
+  if (NB == 2) issue(0);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) settle(S[t]);
+  for (int c = 0; c < nc; ++c) {
+    if (NB == 2) vm_wait<0>();
+    wg_barrier();  // (two buffers: this chunk's tiles are there,) the last chunk's are read
+    if (NB == 1) {
+      issue(c);
+      vm_wait<0>();
+      wg_barrier();
+    } else if (c + 1 < nc) {
+      issue(c + 1);
+    }
+    const T(*lds)[kC * DH] = ring[NB == 2 ? c & 1 : 0];
     const int len = min(kC, sg.len - c * kC);
-    float lg2 = lg2h;  // opaque, so that no table of powers is kept in registers
-    asm volatile("" : "+v"(lg2));
-#pragma unroll 1
-    for (int blk = wave; blk < 10; blk += NW) {
+    const unsigned tb = lds_addr(&tab[len < kC][0][4 * lg]);
+    each<NR>([&](auto n) __attribute__((always_inline)) {
+      const int blk = n * NW + wave;
+      if (blk >= 10) return;
       const int ib = blk >= 6 ? 3 : blk >= 3 ? 2 : blk >= 1 ? 1 : 0, jb = blk - ib * (ib + 1) / 2;
       f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
       each<KS>([&](auto ds) __attribute__((always_inline)) {
@@ -528,13 +801,11 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
         s = mma16(kf, TL::take_row(qr, lane), s);
         dp = mma16(vf, TL::take_row(dr, lane), dp);
       });
-      const int i = ib * 16 + lr;
+      if (ib * 16 + lr < len) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int j = jb * 16 + lg * 4 + r;
-        if (j < i && i < len) sum += a.scale * s[r] * dp[r] * (float)(i - j) * powg(lg2, i - j - 1);
+        for (int r = 0; r < 4; ++r) sum += s[r] * dp[r] * fac[n][r];
       }
-    }
+    });
     ColRaw<T> dr[2], vr[2];
     F df[2], vf[2];
     ColBase<T> db = TL::col_base(lds[3], lane), vb = TL::col_base(lds[2], lane);
@@ -550,15 +821,22 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
       df[us] = take(dr[us]);
       vf[us] = take(vr[us]);
     }
-    // weights of the rows this lane holds: row(us, e)
+    // the weights of the rows this lane holds, from table x
     float w[2][8];
-    auto each = [&](auto f) __attribute__((always_inline)) {
+    auto weights = [&](auto x) __attribute__((always_inline)) {
+      f32x4 t[2][2];
+      each<2>([&](auto us) {
+        t[us][0] = lds_read_f32x4_at<(x * kC + us * 32) * 4>(tb);
+        t[us][1] = lds_read_f32x4_at<(x * kC + us * 32 + 16) * 4>(tb);
+      });
+      lds_tr_wait();
 #pragma unroll
       for (int us = 0; us < 2; ++us)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = us * 32 + (e < 4 ? 4 * lg + e : 12 + 4 * lg + e);
-          w[us][e] = j < len ? f(j) : 0.f;
+        for (int hf = 0; hf < 2; ++hf) {
+          lds_tr_bind(t[us][hf]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[us][hf * 4 + e] = t[us][hf][e];
         }
     };
     f32x4 W[NT];
@@ -568,26 +846,38 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) sum += W[t][r] * x[t][r];
     };
+    // scale g^(i+1), then scale (i+1) g^i
+    const ColBase<T> qb = TL::col_base(lds[0], lane), kb = TL::col_base(lds[1], lane);
+    weights(std::integral_constant<int, 0>{});
+#pragma unroll
+    for (int us = 0; us < 2; ++us)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[us][e] *= a.scale * gh;
 #pragma unroll
     for (int t = 0; t < NT; ++t) W[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    each([&](int i) { return a.scale * (float)(i + 1) * powg(lg2, i); });
-    add_outer<T, DH>(W, TL::col_base(lds[0], lane), 0, df, w, true);
-    inner(S);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) W[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    each([&](int i) { return a.scale * powg(lg2, i + 1); });
-    add_outer<T, DH>(W, TL::col_base(lds[0], lane), 0, df, w, true);
+    add_outer<T, DH, 4>(W, qb, 0, df, w, true);
     inner(D);
-    const float g = powg(lg2, len), g1 = (float)len * powg(lg2, len - 1);
+    weights(std::integral_constant<int, 0>{});
+#pragma unroll
+    for (int us = 0; us < 2; ++us)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        w[us][e] *= a.scale * (float)(us * 32 + (e < 4 ? e : 12 + e) + 1 + 4 * lg);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) W[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    add_outer<T, DH, 4>(W, qb, 0, df, w, true);
+    inner(S);
+    const float g = len == kC ? gC : powg(lg2h, len);
+    const float g1 = (float)len * (len == kC ? gC1 : powg(lg2h, len - 1));
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       D[t] = D[t] * g + S[t] * g1;
       S[t] *= g;
     }
-    each([&](int j) { return j < len - 1 ? (float)(len - 1 - j) * powg(lg2, len - 2 - j) : 0.f; });
-    add_outer<T, DH>(D, TL::col_base(lds[1], lane), 0, vf, w, true);
-    each([&](int j) { return powg(lg2, len - 1 - j); });
-    add_outer<T, DH>(S, TL::col_base(lds[1], lane), 0, vf, w, true);
+    weights(std::integral_constant<int, 2>{});
+    add_outer<T, DH, 4>(D, kb, 0, vf, w, true);
+    weights(std::integral_constant<int, 1>{});
+    add_outer<T, DH, 4>(S, kb, 0, vf, w, true);
   }
   const float* R = !sg.last ? a.seg_r + bd + dd : a.ds_out ? a.ds_out + sq : nullptr;
   if (R) {
@@ -658,13 +948,27 @@ __global__ __launch_bounds__(256) void lin_step_kernel(LinStep a) {
   }
 }
 
+template <typename T, int DH> constexpr bool lin_joined = sizeof(T) == 2 && DH <= 64;
+
 template <typename T, int DH>
 hipError_t pass_t(const LinPass& a, bool rev, bool state, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)(a.total / a.seg + a.nseq) * a.H));
-  if (rev && state) lin_kernel<T, DH, true, true><<<grid, DH * 4, 0, s>>>(a);
-  else if (rev) lin_kernel<T, DH, true, false><<<grid, DH * 4, 0, s>>>(a);
-  else if (state) lin_kernel<T, DH, false, true><<<grid, DH * 4, 0, s>>>(a);
-  else lin_kernel<T, DH, false, false><<<grid, DH * 4, 0, s>>>(a);
+  if constexpr (!lin_joined<T, DH>) {
+    if (rev && state) lin_kernel<T, DH, true, true, false><<<grid, DH * 4, 0, s>>>(a);
+    else if (rev) lin_kernel<T, DH, true, false, false><<<grid, DH * 4, 0, s>>>(a);
+  }
+  if (!rev && state) lin_kernel<T, DH, false, true, false><<<grid, DH * 4, 0, s>>>(a);
+  else if (!rev && a.sum_state) {
+    if constexpr (lin_joined<T, DH>) lin_kernel<T, DH, false, false, true><<<grid, DH * 4, 0, s>>>(a);
+  } else if (!rev) {
+    lin_kernel<T, DH, false, false, false><<<grid, DH * 4, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+template <int DH>
+hipError_t dkdv_t(const LinPair& a, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)(a.total / a.seg + a.nseq) * a.H));
+  lin_dkdv_kernel<DH><<<grid, DH * 4, 0, s>>>(a);
   return hipGetLastError();
 }
 template <typename T, int DH>
@@ -696,6 +1000,14 @@ hipError_t lin_scan(int dh, const LinPass& a, bool rev, hipStream_t s) {
                                                 a.s_in, a.seg_state, a.given);
   return hipGetLastError();
 }
+hipError_t lin_dkdv(int dh, const LinPair& a, hipStream_t s) {
+  switch (dh) {
+    case 16: return dkdv_t<16>(a, s);
+    case 32: return dkdv_t<32>(a, s);
+    default: return dkdv_t<64>(a, s);
+  }
+}
+bool lin_joined_backward(DType dt, int dh) { return dt == DType::BF16 && dh <= 64; }
 hipError_t lin_dgamma(DType dt, int dh, const LinDecay& a, hipStream_t s) {
   BY_TYPE_AND_WIDTH(dgamma_t, dt, dh, a, s);
 }

@@ -459,7 +459,9 @@ int bcmt_linattn_backward(const bcmt_linattn_config* cfg, const void* q, const v
     a.out = out;
     a.ldo = lo;
   };
-  // The states between segments: S of k, v in order; R of q, dO in reverse.
+  // The states between segments: S of k, v in order; R of q, dO in reverse
+  // (joined: its sums come with dq).
+  const bool joined = lin_joined_backward(dt, c.dh);
   if (pl.cut) {
     rows(nullptr, 0, k, ldk, v, ldv, nullptr, 0);
     a.s_in = S_in;
@@ -467,25 +469,35 @@ int bcmt_linattn_backward(const bcmt_linattn_config* cfg, const void* q, const v
     a.s_upd = 1.f;
     if (lin_pass(dt, c.dh, a, false, true, s) != hipSuccess) return BCMT_ERR_HIP;
     if (lin_scan(c.dh, a, false, s) != hipSuccess) return BCMT_ERR_HIP;
-    rows(nullptr, 0, q, ldq, dO, ldo, nullptr, 0);
-    a.s_in = dS_out;
-    a.seg_state = seg_r;
-    a.given = given;
-    a.s_upd = c.scale;
-    if (lin_pass(dt, c.dh, a, true, true, s) != hipSuccess) return BCMT_ERR_HIP;
-    if (lin_scan(c.dh, a, true, s) != hipSuccess) return BCMT_ERR_HIP;
   }
   // dq: rows dO, v, k in order, the state transposed.
   rows(dO, ldo, v, ldv, k, ldk, dq, ldq);
-  a.given = nullptr;
-  a.fine = false;
   a.s_in = S_in;
   a.seg_state = seg_s;
   a.sr = 1;
   a.sc = c.dh;
   a.s_intra = a.s_inter = c.scale;
   a.s_upd = 1.f;
+  a.fine = false;
+  if (joined && pl.cut) {
+    a.q = q;
+    a.ldq = ldq;
+    a.sum_state = seg_r;
+    a.s_sum = c.scale;
+  }
   if (lin_pass(dt, c.dh, a, false, false, s) != hipSuccess) return BCMT_ERR_HIP;
+  if (pl.cut) {
+    rows(nullptr, 0, q, ldq, dO, ldo, nullptr, 0);
+    a.s_in = dS_out;
+    a.seg_state = seg_r;
+    a.given = given;
+    a.s_upd = c.scale;
+    a.sr = c.dh;
+    a.sc = 1;
+    a.fine = true;
+    if (!joined && lin_pass(dt, c.dh, a, true, true, s) != hipSuccess) return BCMT_ERR_HIP;
+    if (lin_scan(c.dh, a, true, s) != hipSuccess) return BCMT_ERR_HIP;
+  }
   if (dgamma) {
     LinDecay g{};
     g.q = q;
@@ -512,12 +524,42 @@ int bcmt_linattn_backward(const bcmt_linattn_config* cfg, const void* q, const v
     g.scale = c.scale;
     if (lin_dgamma(dt, c.dh, g, s) != hipSuccess) return BCMT_ERR_HIP;
   }
+  if (joined) {
+    LinPair g{};
+    g.k = k;
+    g.v = v;
+    g.q = q;
+    g.dout = dO;
+    g.dk = dk;
+    g.dv = dv;
+    g.cu = cu;
+    g.gamma = gamma;
+    g.ds_out = dS_out;
+    g.ds_in = dS_in;
+    g.seg_state = seg_r;
+    g.given = given;
+    g.total = c.total;
+    g.nseq = c.nseq;
+    g.H = c.H;
+    g.seg = pl.seg;
+    g.ldk = ldk;
+    g.ldv = ldv;
+    g.ldq = ldq;
+    g.ldo = ldo;
+    g.scale = c.scale;
+    return lin_dkdv(c.dh, g, s) == hipSuccess ? BCMT_OK : BCMT_ERR_HIP;
+  }
   // dk: rows v, dO, q in reverse, the state transposed.
   rows(v, ldv, dO, ldo, q, ldq, dk, ldk);
   a.s_in = dS_out;
   a.seg_state = seg_r;
+  a.given = nullptr;
+  a.sr = 1;
+  a.sc = c.dh;
+  a.s_intra = c.scale;
   a.s_inter = 1.f;
   a.s_upd = c.scale;
+  a.fine = false;
   if (lin_pass(dt, c.dh, a, true, false, s) != hipSuccess) return BCMT_ERR_HIP;
   // dv: rows k, q, dO in reverse; last, since dS_in may be dS_out.
   rows(k, ldk, q, ldq, dO, ldo, dv, ldv);
