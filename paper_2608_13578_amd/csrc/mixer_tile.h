@@ -203,6 +203,51 @@ __device__ __forceinline__ SeqTile find_tile(const int* __restrict__ cu, int nse
   return r;
 }
 
+// Item x of all tiles of all sequences, the ones with the most work first: in
+// descending order of their index (LAST: of the tiles behind them in their
+// sequence), so that no long tile starts when the chip is nearly done.  f(t) = sum
+// over sequences of max(0, tiles - t) items have index >= t; the largest t with
+// f(t) > x is the item's, and among the sequences that have it, x - f(t + 1) counts.
+// Up to 64 sequences, one a lane; more are walked slot by slot.  Items from f(0) on
+// are empty (tile < 0).
+template <bool LAST>
+__device__ __forceinline__ SeqTile find_item(const int* __restrict__ cu, int nseq, int total,
+                                             int TILE, int x) {
+  if (nseq > 64) return find_tile(cu, nseq, total, TILE, LAST ? x : total / TILE + nseq - 1 - x);
+  const int lane = threadIdx.x & 63;
+  int begin = 0, end = 0;
+  if (lane < nseq) {
+    begin = min(max(cu[lane], 0), total);
+    end = min(max(cu[lane + 1], begin), total);
+  }
+  const int n = (end - begin + TILE - 1) / TILE;
+  auto f = [&](int t) {  // (at most total / TILE + 64 tiles: exact in float32 up to 2^24)
+    return (int)wave_sum((float)max(0, n - t));
+  };
+  int lo = 0, hi = (total + TILE - 1) / TILE;  // f(hi) = 0
+  int flo = f(0);
+  SeqTile r{0, 0, 0, -1};
+  if (x >= flo) return r;
+  int fhi = 0;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2, fm = f(mid);
+    if (fm > x) {
+      lo = mid;
+    } else {
+      hi = mid;
+      fhi = fm;
+    }
+  }
+  const unsigned long long has = __ballot(n > lo);
+  const bool mine = n > lo && (int)__popcll(has & ((1ull << lane) - 1)) == x - fhi;
+  const int s = __builtin_ctzll(__ballot(mine));
+  r.seq = s;
+  r.begin = __builtin_amdgcn_readlane(begin, s);
+  r.end = __builtin_amdgcn_readlane(end, s);
+  r.tile = LAST ? __builtin_amdgcn_readlane(n, s) - 1 - lo : lo;
+  return r;
+}
+
 // Nonzero if an element is infinite or NaN (its exponent bits are all ones).
 __device__ __forceinline__ unsigned nonfinite_bits(const bf16x8& v) {
   typedef unsigned u32x4 __attribute__((ext_vector_type(4)));

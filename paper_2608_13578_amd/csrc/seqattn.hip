@@ -91,9 +91,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_fwd_kerne
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int QT = wph * 16 * NQ, hp = NW / wph, HG = H / hp;
-  const int nslot = total / QT + nseq, wq = wave % wph;
+  const int wq = wave % wph;
   const int h = (int)(blockIdx.x % HG) * hp + wave / wph;
-  const SeqTile st = find_tile(cu, nseq, total, QT, nslot - 1 - (int)(blockIdx.x / HG));
+  const SeqTile st = find_item<false>(cu, nseq, total, QT, (int)(blockIdx.x / HG));
   const int bs = st.begin, be = st.end, q0 = bs + st.tile * QT;
   if (st.tile < 0 || q0 >= be) return;
   const int j = h / G;
@@ -304,9 +304,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_dq_kernel
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
   const int QT = wph * 16 * NQ, hp = NW / wph, HG = H / hp;
-  const int nslot = total / QT + nseq, wq = wave % wph;
+  const int wq = wave % wph;
   const int h = (int)(blockIdx.x % HG) * hp + wave / wph;
-  const SeqTile st = find_tile(cu, nseq, total, QT, nslot - 1 - (int)(blockIdx.x / HG));
+  const SeqTile st = find_item<false>(cu, nseq, total, QT, (int)(blockIdx.x / HG));
   const int bs = st.begin, be = st.end, q0 = bs + st.tile * QT;
   if (st.tile < 0 || q0 >= be) return;
   const int j = h / G;
@@ -486,7 +486,7 @@ __global__ __launch_bounds__((KeyShape<T, DH>::NH * 256)) void seq_dkdv_kernel(
   const int lr = lane & 15, lg = lane >> 4;
   const int Hkv = H / G;
   const int j = blockIdx.x % Hkv, pt = blockIdx.x / Hkv % parts;
-  const SeqTile st = find_tile(cu, nseq, total, KT, (int)(blockIdx.x / (Hkv * parts)));
+  const SeqTile st = find_item<true>(cu, nseq, total, KT, (int)(blockIdx.x / (Hkv * parts)));
   const int be = st.end, k0 = st.begin + st.tile * KT;
   if (st.tile < 0 || k0 >= be) return;
   const int heads = G / parts, h0 = j * G + pt * heads;
