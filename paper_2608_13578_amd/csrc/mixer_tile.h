@@ -70,6 +70,8 @@ __device__ __forceinline__ void each(Fn f) {
   each_(f, std::make_integer_sequence<int, N>{});
 }
 
+constexpr int64_t kNearLd = 1 << 24;
+
 template <typename T, int DH>
 struct Tile {
   static constexpr int CH = 16 / (int)sizeof(T);  // elements of a chunk
@@ -93,6 +95,20 @@ struct Tile {
     const int grow = min(r0 + row, rlast);
     __builtin_amdgcn_global_load_lds(src + (int64_t)grow * ld + ((pos ^ swz(row)) * CH),
                                      (lds_void_t*)(t + i * 64 * CH), 16, 0, 0);
+  }
+  // The same loads of whole tiles with the lane's part of the address formed once
+  // (lane_off: bytes from the tile's lowest row, whose address is the wave's): one
+  // vector instruction a load instead of ten.  `down`: row r of the tile is r rows
+  // below its first.  Row strides up to kNearLd, so that a tile's rows are within
+  // 2^32 bytes.
+  __device__ static __forceinline__ unsigned lane_off(int64_t ld, bool down, int i, int lane) {
+    const int id = i * 64 + lane, row = id / NCH, pos = id % NCH;
+    return (unsigned)((down ? 63 - row : row) * (unsigned)ld + (pos ^ swz(row)) * CH) *
+           (unsigned)sizeof(T);
+  }
+  __device__ static __forceinline__ void issue_near(const T* lowest, unsigned off, T* t, int i) {
+    __builtin_amdgcn_global_load_lds((const char*)lowest + off, (lds_void_t*)(t + i * 64 * CH), 16, 0,
+                                     0);
   }
   // The reads of a tile go by a byte address of the lane, formed once, an
   // exclusive or for the columns (a row begins at a multiple of its size, so

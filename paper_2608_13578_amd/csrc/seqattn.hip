@@ -39,19 +39,46 @@ __device__ __forceinline__ typename Frag<T>::type gfrag(const T* p, bool ok) {
 // NW waves (the first 2 NCH of them where there are more waves).
 template <typename T, int DH, int NW>
 constexpr int kPairLoads = 2 * Tile<T, DH>::NCH / NW > 1 ? 2 * Tile<T, DH>::NCH / NW : 1;
-template <typename T, int DH, int NW>
-__device__ __forceinline__ void issue_pair(const T* a, int64_t lda, const T* b, int64_t ldb, int r0,
-                                           int rlast, T* ta, T* tb, int wave, int lane) {
+// NEAR: with the lane's part of the addresses in registers (kept where a kernel has
+// some left; with a single spill in its loop it would wait for memory there).
+template <typename T, int DH, int NW, bool NEAR>
+struct PairLoads {
   typedef Tile<T, DH> TL;
-  constexpr int NI = kPairLoads<T, DH, NW>;
+  static constexpr int NI = kPairLoads<T, DH, NW>;
   static_assert(NI * NW == 2 * TL::NCH || NI == 1, "loads of two tiles");
+  unsigned off[NI];
+  int64_t lda, ldb;
+  int wave, lane;
+  bool near;
+  __device__ __forceinline__ PairLoads(int64_t lda_, int64_t ldb_, int wave_, int lane_)
+      : lda(lda_), ldb(ldb_), wave(wave_), lane(lane_) {
+    near = NEAR && lda <= kNearLd && ldb <= kNearLd;
+    if (!NEAR) return;
 #pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int gi = wave * NI + i;
-    if (gi < TL::NCH) TL::issue(a, lda, r0, rlast, ta, gi, lane);
-    else if (gi < 2 * TL::NCH) TL::issue(b, ldb, r0, rlast, tb, gi - TL::NCH, lane);
+    for (int i = 0; i < NI; ++i) {
+      const int gi = wave * NI + i;
+      off[i] = TL::lane_off(gi < TL::NCH ? lda : ldb, false, gi % TL::NCH, lane);
+    }
   }
-}
+  // Rows r0 .. r0 + 63 of a and b (those behind rlast: rlast's) into ta and tb.
+  __device__ __forceinline__ void operator()(const T* a, const T* b, int r0, int rlast, T* ta,
+                                             T* tb) const {
+    const bool whole = near && r0 + 63 <= rlast;
+    int ln = lane;
+    if (!NEAR) settle(ln);  // (opaque: the addresses are formed anew, not kept)
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int gi = wave * NI + i;
+      if (gi >= 2 * TL::NCH) break;
+      const bool first = gi < TL::NCH;
+      const T* src = first ? a : b;
+      T* t = first ? ta : tb;
+      const int64_t ld = first ? lda : ldb;
+      if (NEAR && whole) TL::issue_near(src + r0 * ld, off[i], t, gi % TL::NCH);
+      else TL::issue(src, ld, r0, rlast, t, gi % TL::NCH, ln);
+    }
+  }
+};
 
 // ------------------------------------------------------------------ forward
 // One workgroup of NW waves, NQ groups of 16 queries each, over NW / wph heads of
@@ -74,10 +101,11 @@ template <typename T, int DH, int NW_> struct QueryShape {
   static constexpr int NW = NW_, NQ = sizeof(T) == 2 ? 2 : 1;
   // buffers of the ring: 128 KB of LDS a workgroup, or 64 KB for two of four waves
   static constexpr int NS = sizeof(T) == 2 ? (DH == 128 && NW == 4 ? 2 : 4) : DH == 128 ? 2 : 3;
+  static constexpr int WAVES = sizeof(T) == 4 ? 1 : 2;  // of a SIMD
 };
 
 template <typename T, int DH, int NW>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_fwd_kernel(
+__global__ __launch_bounds__(NW * 64, (QueryShape<T, DH, NW>::WAVES)) void seq_fwd_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const int* __restrict__ cu, T* __restrict__ o, float* __restrict__ lse, int total, int nseq,
     int H, int G, int wph, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2) {
@@ -86,7 +114,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_fwd_kerne
   constexpr int NQ = QueryShape<T, DH, NW>::NQ, NS = QueryShape<T, DH, NW>::NS;
   constexpr int KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
   constexpr int NI = kPairLoads<T, DH, NW>;
-  constexpr int KUS = sizeof(T) == 2 ? (DH > 64 ? 2 : 4) : 1;  // key groups read at once
+  constexpr int KUS = sizeof(T) == 2 ? 2 : 1;  // key groups read at once
   __shared__ __attribute__((aligned(1024))) T lds[NS][2][64 * DH];
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int lr = lane & 15, lg = lane >> 4;
@@ -231,9 +259,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_fwd_kerne
     });
   };
 
+  const PairLoads<T, DH, NW, (DH <= 64)> load(ldk, ldv, wave, lane);
   auto issue = [&](int it, int buf) __attribute__((always_inline)) {
-    issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + it * 64, kend - 1, lds[buf][0], lds[buf][1], wave,
-                          lane);
+    load(kb, vb, bs + it * 64, kend - 1, lds[buf][0], lds[buf][1]);
   };
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
@@ -287,8 +315,15 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_fwd_kerne
 // The forward's walk again, with delta_t = do_t . o_t formed (and stored for
 // dK/dV) first: s and dp per key tile, dz in place, dQ^T += K^T dZ^T.
 
+// Four waves a workgroup and one a SIMD for 128-wide heads: two would spill.
+template <typename T, int DH, int NW> struct DqShape {
+  static constexpr bool WIDE = sizeof(T) == 2 && DH == 128;
+  static constexpr int NS = WIDE ? 4 : QueryShape<T, DH, NW>::NS;
+  static constexpr int WAVES = WIDE ? 1 : QueryShape<T, DH, NW>::WAVES;
+};
+
 template <typename T, int DH, int NW>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_dq_kernel(
+__global__ __launch_bounds__(NW * 64, (DqShape<T, DH, NW>::WAVES)) void seq_dq_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const int* __restrict__ cu, const T* __restrict__ o, const float* __restrict__ lse,
     const T* __restrict__ dout, T* __restrict__ dq, float* __restrict__ delta, int total, int nseq,
@@ -296,7 +331,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_dq_kernel
     float scale) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
-  constexpr int NQ = QueryShape<T, DH, NW>::NQ, NS = QueryShape<T, DH, NW>::NS;
+  constexpr int NQ = QueryShape<T, DH, NW>::NQ, NS = DqShape<T, DH, NW>::NS;
   constexpr int KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
   constexpr int NI = kPairLoads<T, DH, NW>;
   constexpr int JB = NJ > 4 ? 4 : NJ;  // column operands read at once
@@ -317,9 +352,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void seq_dq_kernel
   for (int nq = 0; nq < NQ; ++nq) tq[nq] = q0 + 16 * (nq & 1 ? 2 * wph - 1 - wq : wq);
   const int kend = min(be, q0 + QT);
   const int nt = (kend - bs + 63) / 64;
+  const PairLoads<T, DH, NW, true> load(ldk, ldv, wave, lane);
   auto issue = [&](int it, int buf) __attribute__((always_inline)) {
-    issue_pair<T, DH, NW>(kb, ldk, vb, ldv, bs + it * 64, kend - 1, lds[buf][0], lds[buf][1], wave,
-                          lane);
+    load(kb, vb, bs + it * 64, kend - 1, lds[buf][0], lds[buf][1]);
   };
 
   F qf[NQ][KS], df[NQ][KS];
@@ -513,12 +548,13 @@ __global__ __launch_bounds__((KeyShape<T, DH>::NH * 256)) void seq_dkdv_kernel(
     }
   }
   constexpr int TILE = 64 * DH;
+  const PairLoads<T, DH, NW, (DH <= 32)> load(ldq, ldo, wave, lane);
   // step it NH + team into a buffer (beyond the last step: the last one again)
   auto issue = [&](int it, int buf) __attribute__((always_inline)) {
     const int step = min(it * NH + team, nstep - 1);
     const int h = h0 + step / nt1, tt = k0 + (step % nt1) * 64;
     T* t = lds + (buf * NH + team) * 2 * TILE;
-    issue_pair<T, DH, NW>(q + h * DH, ldq, dout + h * DH, ldo, tt, be - 1, t, t + TILE, wave, lane);
+    load(q + h * DH, dout + h * DH, tt, be - 1, t, t + TILE);
     const float* src = (wave & 1 ? delta : lse) + (int64_t)h * total + min(tt + lane, be - 1);
     __builtin_amdgcn_global_load_lds(src, (lds_void_t*)rows[buf][team][wave], 4, 0, 0);
   };
@@ -756,7 +792,7 @@ template <typename T, int DH>
 hipError_t bwd_t(const SeqAttn& a, hipStream_t s) {
   const int G = a.H / a.Hkv;
   hipError_t e;
-  if constexpr (sizeof(T) == 2)
+  if constexpr (sizeof(T) == 2 && DH <= 64)
     e = wide_queries(DType::BF16, a) ? dq_nw<T, DH, 8>(a, s) : dq_nw<T, DH, 4>(a, s);
   else
     e = dq_nw<T, DH, 4>(a, s);
