@@ -339,7 +339,7 @@ __global__ __launch_bounds__(DH * 4, sizeof(T) == 2 ? 2 : 1) void lin_kernel(Lin
 #pragma unroll
           for (int ds = 0; ds < KS; ++ds) {
             const F bf = TL::take_row(br[ds], lane);
-            s = mma16(bf, TL::take_row(ar[ds], lane), s);
+            s = TL::mma(bf, TL::take_row(ar[ds], lane), s);
           }
 #pragma unroll
           for (int r = 0; r < 4; ++r) s[r] = fac[n][r] == 0.f ? 0.f : s[r] * fac[n][r];
@@ -573,7 +573,7 @@ __global__ __launch_bounds__(DH * 4, 2) void lin_dkdv_kernel(LinPair a) {
 #pragma unroll
           for (int ds = 0; ds < KS; ++ds) {
             const F bf = TL::take_row(br[ds], lane);
-            s = mma16(bf, TL::take_row(ar[ds], lane), s);
+            s = TL::mma(bf, TL::take_row(ar[ds], lane), s);
           }
 #pragma unroll
           for (int r = 0; r < 4; ++r) s[r] = fac[n][r] == 0.f ? 0.f : s[r] * fac[n][r];
@@ -798,8 +798,8 @@ __global__ __launch_bounds__(DH * 4) void lin_dgamma_kernel(LinDecay a) {
         RowRaw<T> dr = TL::template row_at<ds, 0>(TL::row_base(lds[3], ib * 16 + lr, lane));
         lds_tr_wait();
         const F kf = TL::take_row(kr, lane), vf = TL::take_row(vr, lane);
-        s = mma16(kf, TL::take_row(qr, lane), s);
-        dp = mma16(vf, TL::take_row(dr, lane), dp);
+        s = TL::mma(kf, TL::take_row(qr, lane), s);
+        dp = TL::mma(vf, TL::take_row(dr, lane), dp);
       });
       if (ib * 16 + lr < len) {
 #pragma unroll

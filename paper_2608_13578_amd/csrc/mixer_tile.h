@@ -115,21 +115,49 @@ struct Tile {
   // that the or only permutes its chunks) and a constant offset for the rows.
   //
   // Row operand: elements 32 DS + 8g .. + 7, g = lane / 16, of row r + R; zero
-  // where a row is narrower than a product's 32 columns.
+  // where a row is narrower than a product's 32 columns.  Float32 rows of 16 take
+  // elements 4g .. + 3 instead, and half of the product's instructions (mma).
+  static constexpr bool SHORT = sizeof(T) == 4 && DH == 16;
+  __device__ static __forceinline__ int row_col(int lane) { return (lane >> 4) * (SHORT ? 4 : 8); }
   __device__ static __forceinline__ unsigned row_base(const T* t, int r, int lane) {
-    const int c = (lane >> 4) * 8;
-    return lds_addr(t + off(r, DH >= 32 || c < DH ? c : 0));
+    const int c = row_col(lane);
+    return lds_addr(t + off(r, c < DH ? c : 0));
+  }
+  // The same of a row in global memory (zero if !ok).
+  __device__ static __forceinline__ typename Frag<T>::type row_global(const T* p, int ds, int lane,
+                                                                      bool ok) {
+    typedef typename Frag<T>::type F;
+    const int c = ds * 32 + row_col(lane);
+    if (!ok || c >= DH) return F{};
+    if constexpr (SHORT) {
+      const f32x4 x = load4f(p + c);
+      return F{x[0], x[1], x[2], x[3], 0.f, 0.f, 0.f, 0.f};
+    } else {
+      return load_frag(p + c);
+    }
+  }
+  // Product of two row operands.
+  __device__ static __forceinline__ f32x4 mma(const typename Frag<T>::type& a,
+                                              const typename Frag<T>::type& b, f32x4 c) {
+    if constexpr (SHORT) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+      return c;
+    } else {
+      return mma16(a, b, c);
+    }
   }
   template <int DS, int R>
   __device__ static __forceinline__ RowRaw<T> row_at(unsigned a) {
     constexpr int O = R * DH * (int)sizeof(T);
     if constexpr (sizeof(T) == 2) return {lds_read_b128_at<O>(a ^ (DS * 64))};
+    else if constexpr (SHORT) return {lds_read_f32x4_at<O>(a), f32x4{0.f, 0.f, 0.f, 0.f}};
     else return {lds_read_f32x4_at<O>(a ^ (DS * 128)), lds_read_f32x4_at<O>(a ^ (DS * 128 + 16))};
   }
   __device__ static __forceinline__ typename Frag<T>::type take_row(RowRaw<T>& r, int lane) {
     typedef typename Frag<T>::type F;
     const F f = take(r);
-    return DH >= 32 || (lane >> 4) * 8 < DH ? f : F{};
+    return DH >= 32 || SHORT || (lane >> 4) * 8 < DH ? f : F{};
   }
   // Column operand: column 16 JJ + lane % 16 of rows B0 + 4g .. + 3 and
   // B1 + 4g .. + 3: the order in which two 16-row result tiles hold their rows.

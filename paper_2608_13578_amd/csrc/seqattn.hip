@@ -29,12 +29,6 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-template <typename T>
-__device__ __forceinline__ typename Frag<T>::type gfrag(const T* p, bool ok) {
-  typedef typename Frag<T>::type F;
-  return ok ? load_frag(p) : F{};
-}
-
 // The two tiles (K, V or Q, dO) of one step, 2 NCH wave instructions shared by
 // NW waves (the first 2 NCH of them where there are more waves).
 template <typename T, int DH, int NW>
@@ -140,8 +134,8 @@ __global__ __launch_bounds__(NW * 64, (QueryShape<T, DH, NW>::WAVES)) void seq_f
   for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
     for (int ds = 0; ds < KS; ++ds) {
-      const int t = tq[nq] + lr, c = ds * 32 + lg * 8;
-      qf[nq][ds] = gfrag(q + (int64_t)t * ldq + h * DH + c, t < be && c < DH);
+      const int t = tq[nq] + lr;
+      qf[nq][ds] = TL::row_global(q + (int64_t)t * ldq + h * DH, ds, lane, t < be);
     }
   f32x4 oa[NQ][NJ];
   float m[NQ], l[NQ];
@@ -182,7 +176,7 @@ __global__ __launch_bounds__(NW * 64, (QueryShape<T, DH, NW>::WAVES)) void seq_f
           s[nq][k0 + ku] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int ds = 0; ds < KS; ++ds)
-            s[nq][k0 + ku] = mma16(kf[ds], qf[nq][ds], s[nq][k0 + ku]);
+            s[nq][k0 + ku] = TL::mma(kf[ds], qf[nq][ds], s[nq][k0 + ku]);
         }
       }
     });
@@ -365,11 +359,9 @@ __global__ __launch_bounds__(NW * 64, (DqShape<T, DH, NW>::WAVES)) void seq_dq_k
     float part = 0.f;
 #pragma unroll
     for (int ds = 0; ds < KS; ++ds) {
-      const int c = ds * 32 + lg * 8;
-      const bool ok = t < be && c < DH;
-      qf[nq][ds] = gfrag(q + (int64_t)t * ldq + h * DH + c, ok);
-      df[nq][ds] = gfrag(dout + (int64_t)t * ldo + h * DH + c, ok);
-      const F of = gfrag(o + (int64_t)t * ldo + h * DH + c, ok);
+      qf[nq][ds] = TL::row_global(q + (int64_t)t * ldq + h * DH, ds, lane, t < be);
+      df[nq][ds] = TL::row_global(dout + (int64_t)t * ldo + h * DH, ds, lane, t < be);
+      const F of = TL::row_global(o + (int64_t)t * ldo + h * DH, ds, lane, t < be);
 #pragma unroll
       for (int e = 0; e < 8; ++e) part += to_f32(df[nq][ds][e]) * to_f32(of[e]);
     }
@@ -417,8 +409,8 @@ __global__ __launch_bounds__(NW * 64, (DqShape<T, DH, NW>::WAVES)) void seq_dq_k
           f32x4 sv = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int ds = 0; ds < KS; ++ds) {
-            sv = mma16(kf[ds], qf[nq][ds], sv);
-            dp = mma16(vf[ds], df[nq][ds], dp);
+            sv = TL::mma(kf[ds], qf[nq][ds], sv);
+            dp = TL::mma(vf[ds], df[nq][ds], dp);
           }
           const int t_eff = min(tq[nq] + lr, be - 1);
 #pragma unroll
@@ -537,9 +529,8 @@ __global__ __launch_bounds__((KeyShape<T, DH>::NH * 256)) void seq_dkdv_kernel(
     const int u = uk[nk] + lr;
 #pragma unroll
     for (int ds = 0; ds < KS; ++ds) {
-      const int c = ds * 32 + lg * 8;
-      kf[nk][ds] = gfrag(k + (int64_t)u * ldk + j * DH + c, u < be && c < DH);
-      vf[nk][ds] = gfrag(v + (int64_t)u * ldv + j * DH + c, u < be && c < DH);
+      kf[nk][ds] = TL::row_global(k + (int64_t)u * ldk + j * DH, ds, lane, u < be);
+      vf[nk][ds] = TL::row_global(v + (int64_t)u * ldv + j * DH, ds, lane, u < be);
     }
 #pragma unroll
     for (int jj = 0; jj < NJ; ++jj) {
@@ -599,8 +590,8 @@ __global__ __launch_bounds__((KeyShape<T, DH>::NH * 256)) void seq_dkdv_kernel(
           f32x4 sv = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int ds = 0; ds < KS; ++ds) {
-            sv = mma16(qf[ds], kf[nk][ds], sv);
-            dp = mma16(df[ds], vf[nk][ds], dp);
+            sv = TL::mma(qf[ds], kf[nk][ds], sv);
+            dp = TL::mma(df[ds], vf[nk][ds], dp);
           }
           const int u = uk[nk] + lr;
 #pragma unroll
@@ -863,10 +854,8 @@ __global__ __launch_bounds__((DecShape<T, DH>::NW * 64)) void dec_part_kernel(De
 
   F qf[KS];
 #pragma unroll
-  for (int ds = 0; ds < KS; ++ds) {
-    const int c = ds * 32 + lg * 8;
-    qf[ds] = gfrag((const T*)a.q + (int64_t)b * a.ldq + h * DH + c, hok && c < DH);
-  }
+  for (int ds = 0; ds < KS; ++ds)
+    qf[ds] = TL::row_global((const T*)a.q + (int64_t)b * a.ldq + h * DH, ds, lane, hok);
   float m = -INFINITY, l = 0.f;
   f32x4 oa[NJ];
 #pragma unroll
@@ -917,7 +906,7 @@ __global__ __launch_bounds__((DecShape<T, DH>::NW * 64)) void dec_part_kernel(De
       lds_tr_wait();
       s[ku] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ds = 0; ds < KS; ++ds) s[ku] = mma16(TL::take_row(kr[ds], lane), qf[ds], s[ku]);
+      for (int ds = 0; ds < KS; ++ds) s[ku] = TL::mma(TL::take_row(kr[ds], lane), qf[ds], s[ku]);
     });
     each<NJ>([&](auto jj) { vr[jj] = TL::template col_at<jj, 0, 16>(vcol, ba); });
     float mx = -INFINITY;
