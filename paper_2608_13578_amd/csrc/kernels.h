@@ -456,7 +456,7 @@ bool lin_joined_backward(DType dt, int dh);
 hipError_t lin_pass(DType dt, int dh, const LinPass& a, bool rev, bool state, hipStream_t s);
 // Those sums -> the states at the boundaries between segments (s_in unswapped).
 hipError_t lin_scan(int dh, const LinPass& a, bool rev, hipStream_t s);
-int lin_segment_rows(int total, int nseq, int H, int dh);
+int lin_segment_rows(DType dt, int total, int nseq, int H, int dh);
 
 struct LinDecay {
   const void *q, *k, *v, *dout;

@@ -169,13 +169,21 @@ __device__ __forceinline__ LinSeg lin_segment(const int* cu, int nseq, int total
   return r;
 }
 
-// Buffers of the chunks' tiles: as many as give two workgroups of a CU (one of
-// 128-wide heads) their LDS.  A chunk takes less time than its rows take to come
-// from memory, so two chunks are requested ahead.
+// A workgroup takes as many heads side by side as make 256 bytes of a row, so that
+// memory sees that much of a row at once: 131072 rows of 16 heads of 64 take 362 us
+// with two heads to a workgroup, 431 with one (whose passes run at 3.9 TB/s; the same
+// data as rows of one or two heads at 4.9).
+template <typename T, int DH> constexpr int lin_heads = DH * sizeof(T) < 256 ? 256 / (DH * sizeof(T)) : 1;
+
+// Buffers of the chunks' tiles: what the LDS of a CU holds besides the scores, up to
+// three (two and three measured alike where both fit), and two for the sums, of which
+// a CU then holds two workgroups.
 template <typename T, int DH>
-constexpr int lin_buffers(bool state) {
-  const int row = (int)sizeof(T) * DH;
-  return state ? (row > 256 ? 2 : row == 256 ? 4 : 3) : row > 256 ? 1 : sizeof(T) == 4 && DH >= 32 ? 2 : 3;
+constexpr int lin_buffers(int tiles, bool state) {
+  const int set = tiles * kC * DH * (int)sizeof(T) * lin_heads<T, DH>;
+  const int scores = state ? 0 : kC * kC * (int)sizeof(T) * lin_heads<T, DH>;
+  const int n = (163840 - scores) / set;
+  return state ? 2 : n > 3 ? 3 : n < 1 ? 1 : n;
 }
 
 // ------------------------------------------------------------------ the operator
@@ -185,24 +193,27 @@ constexpr int lin_buffers(bool state) {
 // the local index runs forward, so the sum needs no decay, only falling weights.
 
 template <typename T, int DH, bool REV, bool STATE, bool SUM>
-__global__ __launch_bounds__(DH * 4, sizeof(T) == 2 ? 2 : 1) void lin_kernel(LinPass a) {
+__global__ __launch_bounds__((DH * 4 * lin_heads<T, DH>), sizeof(T) == 2 ? (STATE && DH < 128 ? 4 : 2) : 1)
+void lin_kernel(LinPass a) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
   typedef Tile<T, kC> TP;
   constexpr int NW = DH / 16, NT = DH / 16, KS = DH >= 32 ? DH / 32 : 1;
   constexpr int FIRST = STATE ? 1 : 0;  // tiles a, b, c: the sum needs b and c
   constexpr int TILES = SUM ? 4 : 3 - FIRST;
-  constexpr int NB = SUM ? 2 : lin_buffers<T, DH>(STATE);
+  constexpr int HP = lin_heads<T, DH>, NB = lin_buffers<T, DH>(TILES, STATE);
   constexpr int NI = TL::NCH / NW;  // loads of a tile by each wave
-  __shared__ __attribute__((aligned(1024))) T lds[NB][TILES][kC * DH];
-  __shared__ __attribute__((aligned(1024))) T P[STATE ? 16 : kC * kC];
-  const int lane = threadIdx.x & 63, wave = wave_index();
+  __shared__ __attribute__((aligned(1024))) T lds_all[HP][NB][TILES][kC * DH];
+  __shared__ __attribute__((aligned(1024))) T P_all[HP][STATE ? 16 : kC * kC];
+  // NW waves a head; a head behind the last one repeats it and writes nothing
+  const int lane = threadIdx.x & 63, wave = wave_index() % NW, hw = wave_index() / NW;
   const int lr = lane & 15, lg = lane >> 4;
-  const int h = blockIdx.x % a.H;
-  // The pass over the segments' sums walks them in order, the operator backwards:
-  // it begins with the rows that were read last and are still in the cache.
-  const int slot = blockIdx.x / a.H, nslot = a.total / a.seg + a.nseq;
-  const LinSeg sg = lin_segment(a.cu, a.nseq, a.total, a.seg, STATE ? slot : nslot - 1 - slot);
+  const int HG = (a.H + HP - 1) / HP, hx = (int)(blockIdx.x % HG) * HP + hw;
+  const bool alive = hx < a.H;
+  const int h = alive ? hx : a.H - 1;
+  T(*lds)[TILES][kC * DH] = lds_all[hw];
+  T* P = P_all[hw];
+  const LinSeg sg = lin_segment(a.cu, a.nseq, a.total, a.seg, blockIdx.x / HG);
   if (sg.len < 0) return;
   // the sum of a segment that no other follows is not needed
   if (STATE && (REV ? sg.t0 == 0 : sg.last)) return;
@@ -432,7 +443,7 @@ __global__ __launch_bounds__(DH * 4, sizeof(T) == 2 ? 2 : 1) void lin_kernel(Lin
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib) {
         const int i = ib * 16 + lr;
-        if (i < len)
+        if (alive && i < len)
           store4((T*)a.out + (r0 + (REV ? -1 : 1) * (int64_t)(c * kC + i)) * a.ldo + h * DH +
                      wave * 16 + lg * 4,
                  oa[ib][0], oa[ib][1], oa[ib][2], oa[ib][3]);
@@ -441,6 +452,7 @@ __global__ __launch_bounds__(DH * 4, sizeof(T) == 2 ? 2 : 1) void lin_kernel(Lin
     buf = buf + 1 == NB ? 0 : buf + 1;
     next = next + 1 == NB ? 0 : next + 1;
   }
+  if (!alive) return;
   if constexpr (SUM) {
     if (sg.t0 > 0)
       store_state<NT>(R, a.sum_state + sg.bound * dd + (int64_t)h * DH * DH, DH, 1, col, lg);
@@ -952,16 +964,17 @@ template <typename T, int DH> constexpr bool lin_joined = sizeof(T) == 2 && DH <
 
 template <typename T, int DH>
 hipError_t pass_t(const LinPass& a, bool rev, bool state, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)(a.total / a.seg + a.nseq) * a.H));
+  constexpr int HP = lin_heads<T, DH>, BS = DH * 4 * HP;
+  const dim3 grid((unsigned)((int64_t)(a.total / a.seg + a.nseq) * ((a.H + HP - 1) / HP)));
   if constexpr (!lin_joined<T, DH>) {
-    if (rev && state) lin_kernel<T, DH, true, true, false><<<grid, DH * 4, 0, s>>>(a);
-    else if (rev) lin_kernel<T, DH, true, false, false><<<grid, DH * 4, 0, s>>>(a);
+    if (rev && state) lin_kernel<T, DH, true, true, false><<<grid, BS, 0, s>>>(a);
+    else if (rev) lin_kernel<T, DH, true, false, false><<<grid, BS, 0, s>>>(a);
   }
-  if (!rev && state) lin_kernel<T, DH, false, true, false><<<grid, DH * 4, 0, s>>>(a);
+  if (!rev && state) lin_kernel<T, DH, false, true, false><<<grid, BS, 0, s>>>(a);
   else if (!rev && a.sum_state) {
-    if constexpr (lin_joined<T, DH>) lin_kernel<T, DH, false, false, true><<<grid, DH * 4, 0, s>>>(a);
+    if constexpr (lin_joined<T, DH>) lin_kernel<T, DH, false, false, true><<<grid, BS, 0, s>>>(a);
   } else if (!rev) {
-    lin_kernel<T, DH, false, false, false><<<grid, DH * 4, 0, s>>>(a);
+    lin_kernel<T, DH, false, false, false><<<grid, BS, 0, s>>>(a);
   }
   return hipGetLastError();
 }
@@ -1015,15 +1028,14 @@ hipError_t lin_step(DType dt, int dh, const LinStep& a, hipStream_t s) {
   BY_TYPE_AND_WIDTH(step_t, dt, dh, a, s);
 }
 
-// Rows of a segment: such that the workgroups, at most total / seg + nseq of a
-// head, are one round of those that the chip holds at once (two of four waves to
-// a CU at 64 columns), or, with many sequences, a quarter of it more than these.
-// Two rounds of half the rows ran the second one with a third of the chip (131072
-// rows in 3 sequences, 16 heads of 64: the sums of 1056 segments 138 us, of 528
-// 113 us).  At least 256 rows: a boundary's state, written twice and read twice,
-// costs the traffic of a few chunks.
-int lin_segment_rows(int total, int nseq, int H, int dh) {
-  const int round = 32768 / dh / H;  // segments of a head
+// Rows of a segment: such that the workgroups, at most total / seg + nseq of a group
+// of heads, are one round of those that the chip holds at once (one of eight waves
+// to a CU), or, with many sequences, a quarter of it more than these.  At least 256
+// rows: a boundary's state, written twice and read twice, costs the traffic of a few
+// chunks.
+int lin_segment_rows(DType dt, int total, int nseq, int H, int dh) {
+  const int row = dh * (dt == DType::BF16 ? 2 : 4), hp = row < 256 ? 256 / row : 1;
+  const int round = 256 / ((H + hp - 1) / hp);  // segments of a group of heads
   int n = round - nseq;
   if (n < round / 4) n = round / 4;
   if (n < 1) n = 1;

@@ -138,7 +138,7 @@ struct LinPlan {
   bool cut;  // whether a sequence can have more than one segment
   size_t fwd, rev, given, part, fwd_bytes, bwd_bytes;
   explicit LinPlan(const bcmt_linattn_config& c) {
-    seg = lin_segment_rows(c.total, c.nseq, c.H, c.dh);
+    seg = lin_segment_rows(dtype_of(c.dtype), c.total, c.nseq, c.H, c.dh);
     cut = seg < c.total;
     if (!cut) seg = (c.total + 63) / 64 * 64;
     nslot = c.total / seg + c.nseq;
