@@ -735,7 +735,8 @@ int64_t query_grid(int NW, int NQ, const SeqAttn& a) {
   return (int64_t)(a.total / (wph * 16 * NQ) + a.nseq) * (a.H * wph / NW);
 }
 // Eight waves a workgroup (less traffic per query) once they make four rounds
-// over the CUs, else four.
+// over the CUs, else four (16 heads of 128 on 2, forward, 8 against 4 waves: 4096
+// rows 145 and 121 us, 16384 rows 624 and 685, 32768 rows 4.74 and 5.38 ms).
 bool wide_queries(DType dt, const SeqAttn& a) {
   return dt == DType::BF16 && query_grid(8, 2, a) >= 1024;
 }
@@ -768,7 +769,9 @@ hipError_t fwd_t(const SeqAttn& a, hipStream_t s) {
 }
 
 // Parts of a group's heads for dK and dV: a divisor of G, until there are two
-// workgroups for every CU.
+// workgroups for every CU (the whole gradient of four sequences of 2048, 16 heads of
+// 64 on 4: 196 us, 213 with four, 244 with one, 247 with no parts; of one sequence of
+// 4096, 16 heads of 128 on 2: 401, 403, 574 and 1747).
 int head_parts(int64_t tiles, int Hkv, int G) {
   int p = 1;
   while (p < G && (G % p || tiles * Hkv * p < 512)) ++p;
@@ -990,32 +993,72 @@ __global__ __launch_bounds__((DecShape<T, DH>::NW * 64)) void dec_part_kernel(De
   }
 }
 
-// Joins the parts of one (sequence, head): DH / 4 lanes each.
+// Joins the parts of one (sequence, head): DH / 4 lanes for the columns, as many
+// groups of them as a workgroup has take the parts in turn, eight loads at a time
+// (one sequence of 32768 positions, 4 heads of 64, 128 parts: 13 us for the step,
+// 52 with the parts one after another).
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void dec_join_kernel(DecAttn a) {
-  constexpr int KT = DecShape<T, DH>::KT, PER = 256 / (DH / 4);
-  const int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / (DH / 4);
-  if (row >= (int64_t)a.B * a.H) return;
-  const int b = (int)(row / a.H), h = (int)(row % a.H), c = (threadIdx.x % (DH / 4)) * 4;
+  constexpr int KT = DecShape<T, DH>::KT, L = DH / 4, AT = 8;
+  __shared__ __attribute__((aligned(16))) float acc_of[256 / L][DH];
+  __shared__ float m_of[256 / L], l_of[256 / L];
+  const int row = blockIdx.x, b = row / a.H, h = row % a.H;
+  const int ng = blockDim.x / L, gi = threadIdx.x / L, c = (threadIdx.x % L) * 4;
   const int slot = a.slot ? a.slot[b] : b, n = a.length[b];
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float inv = 0.f;
-  if (slot >= 0 && slot < a.slots && n >= 0 && n < a.cap) {
-    const int ntile = n / KT + 1, per = (ntile + a.nsplit - 1) / a.nsplit;
-    const int np = (ntile + per - 1) / per;
-    const float* ml = a.part_ml + row * a.nsplit * 2;
-    float m = -INFINITY, l = 0.f;
-    for (int p = 0; p < np; ++p) m = fmaxf(m, ml[2 * p]);
-    const float ms = m == -INFINITY ? 0.f : m;
-    for (int p = 0; p < np; ++p) {
-      const float w = exp2_fast(ml[2 * p] - ms);
-      l += w * ml[2 * p + 1];
-      acc += w * *(const f32x4*)(a.part_o + (row * a.nsplit + p) * DH + c);
-    }
-    inv = 1.0f / l;
+  T* o = (T*)a.o + (int64_t)b * a.ldo + h * DH + c;
+  if (slot < 0 || slot >= a.slots || n < 0 || n >= a.cap) {
+    if (gi == 0) store4(o, 0.f, 0.f, 0.f, 0.f);
+    return;
   }
-  store4((T*)a.o + (int64_t)b * a.ldo + h * DH + c, acc[0] * inv, acc[1] * inv, acc[2] * inv,
-         acc[3] * inv);
+  const int ntile = n / KT + 1, per = (ntile + a.nsplit - 1) / a.nsplit;
+  const int np = (ntile + per - 1) / per;
+  const float* ml = a.part_ml + (int64_t)row * a.nsplit * 2;
+  const float* po = a.part_o + (int64_t)row * a.nsplit * DH + c;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  for (int p0 = gi; p0 < np; p0 += ng * AT) {
+    f32x4 x[AT];
+    float mx[AT], lx[AT], mn = m;
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const int p = min(p0 + i * ng, np - 1);  // one behind the last has no weight
+      mx[i] = ml[2 * p];
+      lx[i] = ml[2 * p + 1];
+      x[i] = *(const f32x4*)(po + (int64_t)p * DH);
+    }
+#pragma unroll
+    for (int i = 0; i < AT; ++i) mn = fmaxf(mn, mx[i]);
+    const float ms = mn == -INFINITY ? 0.f : mn, old = exp2_fast(m - ms);
+    l *= old;
+    acc *= old;
+#pragma unroll
+    for (int i = 0; i < AT; ++i)
+      if (p0 + i * ng < np) {
+        const float w = exp2_fast(mx[i] - ms);
+        l += w * lx[i];
+        acc += w * x[i];
+      }
+    m = mn;
+  }
+  *(f32x4*)&acc_of[gi][c] = acc;
+  if (c == 0) {
+    m_of[gi] = m;
+    l_of[gi] = l;
+  }
+  __syncthreads();
+  if (gi != 0) return;
+  m = -INFINITY;
+  for (int i = 0; i < ng; ++i) m = fmaxf(m, m_of[i]);
+  const float ms = m == -INFINITY ? 0.f : m;
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  l = 0.f;
+  for (int i = 0; i < ng; ++i) {
+    const float w = exp2_fast(m_of[i] - ms);
+    l += w * l_of[i];
+    acc += w * *(const f32x4*)&acc_of[i][c];
+  }
+  const float inv = 1.0f / l;
+  store4(o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
 template <typename T, int DH>
@@ -1025,8 +1068,8 @@ hipError_t dec_t(const DecAttn& a, hipStream_t s) {
   dec_part_kernel<T, DH><<<dim3(a.nsplit, a.B * a.Hkv * NH), NW * 64, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
-  constexpr int PER = 256 / (DH / 4);
-  dec_join_kernel<T, DH><<<dim3((unsigned)(((int64_t)a.B * a.H + PER - 1) / PER)), 256, 0, s>>>(a);
+  // a wave for each row, or four where it has many parts
+  dec_join_kernel<T, DH><<<dim3((unsigned)(a.B * a.H)), a.nsplit > 16 ? 256 : 64, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -1045,13 +1088,16 @@ hipError_t seq_attn_decode(DType dt, int dh, const DecAttn& a, hipStream_t s) {
   BY_TYPE_AND_WIDTH(dec_t, dt, dh, a, s);
 }
 
-// Parts of the cache: enough workgroups for four per CU, at least two tiles of
-// every wave in a part.
+// Parts of the cache: enough workgroups for four per CU, so that sequences of
+// different lengths even out (32 of up to 8192 positions, 8 heads of 128: 111 us,
+// 119 with two or eight per CU; 32 of 4096 each: 106, 105 and 119), at least two
+// tiles of every wave in a part, and no more parts than CUs, since the join reads
+// them all (one sequence of 131072, one head: 23 us with 256, 32 with 512).
 int seq_attn_decode_splits(DType dt, int dh, int B, int H, int Hkv, int cap) {
   const int G = H / Hkv, NH = (G + 15) / 16;
   const int nw = (dt == DType::BF16 ? 2 : 4) * dh >= 512 ? 2 : 4;
   const int64_t wgs = (int64_t)B * Hkv * NH;
-  const int64_t want = (1024 + wgs - 1) / wgs, most = (cap + nw * 64 - 1) / (nw * 64);
+  const int64_t want = wgs < 4 ? 256 : (1024 + wgs - 1) / wgs, most = (cap + nw * 64 - 1) / (nw * 64);
   const int64_t n = want < most ? want : most;
   return n < 1 ? 1 : (int)n;
 }
