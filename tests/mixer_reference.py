@@ -84,6 +84,22 @@ def attention(q, k, v, cu, scale, dtype, do=None):
     return {n: tuple(x) for n, x in res.items()}
 
 
+def token(q, k, v, scale, dtype):
+    """The last row of a sequence: q [H, dh], k, v [n, Hkv, dh].  (value, bound) as
+    of `attention`."""
+    (H, dh), (n, Hkv, _), u = q.shape, k.shape, unit(dtype)
+    val, bound = torch.zeros_like(q), torch.zeros_like(q)
+    for h in range(H):
+        K, V = k[:, h * Hkv // H], v[:, h * Hkv // H]
+        z, zabs = scale * K @ q[h], scale * K.abs() @ q[h].abs()
+        lse = torch.logsumexp(z, 0)
+        p = torch.exp(z - lse)
+        ep = E * ((dh + 8) * (zabs + zabs.max()) + 4 * lse.abs() + n + 16)
+        val[h] = p @ V
+        bound[h] = (p * (u + ep)) @ V.abs() + (n + 64) * E * (p @ V.abs()) + u * val[h].abs()
+    return val, bound
+
+
 def linear(q, k, v, gamma, cu, scale, dtype, S_in=None, do=None, dS_out=None):
     """q, k, v, do [total, H, dh], gamma [H], states [nseq, H, dh, dh], float64.
     {name: (value, bound)} from the quadratic form."""

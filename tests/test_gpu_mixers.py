@@ -696,3 +696,165 @@ def test_tensors_that_do_not_fit_are_refused(torch_cuda):
     with pytest.raises(ValueError):
         lin.forward(q, q.clone(), q.clone(), torch.ones(2, device="cuda"), c, o,
                     torch.zeros(1, 2, 64, 32, device="cuda"))
+
+
+# Batches with workgroups for the whole chip several times over, where the kernels
+# take more waves a workgroup and split no group of heads, or only in part.
+ATTN_MANY = [
+    ("bf16", 64, 16, 4, [(37 * i) % 131 for i in range(220)], 0, 0, True, 1.0),
+    ("bf16", 32, 16, 16, [(53 * i) % 301 for i in range(64)], 1, 2, False, 1.0),
+    ("bf16", 16, 32, 8, [(29 * i) % 71 for i in range(200)], 0, 3, False, 4.0),
+    ("bf16", 128, 16, 2, [(41 * i) % 140 for i in range(220)], 2, 0, False, 1.0),
+    ("bf16", 64, 16, 1, [(29 * i) % 71 for i in range(90)], 0, 0, False, 1.0),
+    ("f32", 64, 8, 4, [(23 * i) % 61 for i in range(150)], 0, 1, True, 1.0),
+]
+
+
+@pytest.mark.parametrize("case", ATTN_MANY,
+                         ids=lambda c: f"{c[0]}-dh{c[1]}-H{c[2]}.{c[3]}-{len(c[4])}sequences")
+def test_attention_of_many_sequences(torch_cuda, case):
+    test_attention(torch_cuda, case)
+
+
+LONG_CACHES = [
+    # dtype, dh, cap, H, Hkv, lengths
+    ("bf16", 64, 20000, 4, 2, [19999]),
+    ("bf16", 16, 9000, 3, 1, [8999, 300]),
+    ("bf16", 32, 9000, 2, 2, [4500, 9000]),
+    ("bf16", 128, 70001, 1, 1, [70000]),
+    ("f32", 128, 5000, 2, 1, [4321, 0]),
+    ("f32", 32, 6000, 2, 2, [5999]),
+]
+
+
+@pytest.mark.parametrize("case", LONG_CACHES, ids=lambda c: f"{c[0]}-dh{c[1]}-cap{c[2]}")
+def test_attention_decode_of_long_caches(torch_cuda, case):
+    """Caches in many parts, joined by more lanes."""
+    from paper_2608_13578_amd.mixers import AttentionDecoder
+    dtype, dh, cap, H, Hkv, lens = case
+    say(f"decode {case}")
+    g, B = rng(13), len(lens)
+    q, k, v = (normal(g, B, h, dh, dtype=dtype) for h in (H, Hkv, Hkv))
+    kc, vc = (normal(g, B, cap, Hkv, dh, dtype=dtype) for _ in range(2))
+    d = AttentionDecoder(B, B, cap, H, Hkv, dh, dtype)
+    o = torch.full((B, H, dh), 7.0, dtype=DT[dtype], device="cuda")
+    args = (dev(q, dtype), dev(k, dtype), dev(v, dtype), None, i32(lens), dev(kc, dtype), dev(vc, dtype))
+    d.step(*args, o)
+    again = torch.empty_like(o)
+    d.step(*args, again)
+    torch.cuda.synchronize()
+    assert torch.equal(o, again)
+    for b, n in enumerate(lens):
+        if n >= cap:
+            assert bool((o[b] == 0).all())
+            continue
+        ref.within(f"o[{b}]", o[b], ref.token(q[b], torch.cat([kc[b, :n], k[b][None]]),
+                                              torch.cat([vc[b, :n], v[b][None]]), dh ** -0.5, dtype))
+
+
+def test_gradients_with_rows_far_apart(torch_cuda):
+    """Rows more than 2^25 bytes apart, gradients among them."""
+    from paper_2608_13578_amd.mixers import LinearAttention, PackedAttention
+    dh, total, ld = 64, 150, (1 << 24) + 64
+    room = torch.empty((total - 1) * ld + 6 * dh, dtype=torch.bfloat16, device="cuda")
+    parts = [room.as_strided((total, dh), (ld, 1), i * dh) for i in range(6)]
+    g, cu, scale = rng(14), [0, 81, 150], dh ** -0.5
+    q, k, v, do = (normal(g, total, 1, dh, dtype="bf16") for _ in range(4))
+    for p, x in zip(parts, (q, k, v)):
+        p.copy_(dev(x[:, 0], "bf16"))
+    ins, grads, c, dod = parts[:3], parts[3:], i32(cu), dev(do, "bf16")
+    o = torch.empty(total, 1, dh, dtype=torch.bfloat16, device="cuda")
+    att = PackedAttention(total, 2, 1, 1, dh, ldq=ld, ldk=ld, ldv=ld)
+    lse = att.new_lse()
+    att.forward(*ins, c, o, lse)
+    att.backward(*ins, c, o, lse, dod, *grads)
+    torch.cuda.synchronize()
+    want = ref.attention(q, k, v, cu, scale, "bf16", do)
+    for n, x in zip(("o", "dq", "dk", "dv"), (o, *grads)):
+        ref.within(n, x, want[n])
+    la = LinearAttention(total, 2, 1, dh, ldq=ld, ldk=ld, ldv=ld)
+    gam = torch.tensor([0.97])
+    la.forward(*ins, gam.cuda(), c, o)
+    la.backward(*ins, gam.cuda(), c, dod, *grads)
+    torch.cuda.synchronize()
+    want = ref.linear(q, k, v, gam.double(), cu, scale, "bf16", None, do)
+    for n, x in zip(("o", "dq", "dk", "dv"), (o, *grads)):
+        ref.within(n, x, want[n])
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("f32", 32), ("bf16", 128)])
+def test_linear_attention_with_a_negative_scale(torch_cuda, dtype, dh):
+    from paper_2608_13578_amd.mixers import LinearAttention
+    H, cu, scale = 2, [0, 300, 377], -0.7
+    g, total = rng(15), 377
+    q, k, v, do = (normal(g, total, H, dh, dtype=dtype) for _ in range(4))
+    gam = torch.tensor([0.9, 0.99])
+    want = ref.linear(q, k, v, gam.double(), cu, scale, dtype, None, do)
+    la = LinearAttention(total, 2, H, dh, dtype, scale=scale)
+    x = [dev(t, dtype) for t in (q, k, v, do)]
+    o, dq, dk, dv = (torch.empty_like(x[0]) for _ in range(4))
+    S, dS, dg = la.new_state(), la.new_state(), torch.empty(H, device="cuda")
+    la.forward(*x[:3], gam.cuda(), i32(cu), o, None, S)
+    la.backward(*x[:3], gam.cuda(), i32(cu), x[3], dq, dk, dv, None, None, dS, dg)
+    torch.cuda.synchronize()
+    for n, y in (("o", o), ("S", S), ("dq", dq), ("dk", dk), ("dv", dv), ("dS", dS), ("dgamma", dg)):
+        ref.within(n, y, want[n])
+
+
+def test_states_past_32_bits(torch_cuda):
+    """A pool of states of more than 2^33 bytes."""
+    from paper_2608_13578_amd.mixers import LinearAttentionDecoder
+    H, dh, slots = 16, 128, 8200
+    pool = torch.empty(slots, H, dh, dh, device="cuda")
+    g = rng(16)
+    slot = [slots - 1, 0, slots // 2 + 5]
+    S = normal(g, 3, H, dh, dh)
+    pool[slot] = S.float().cuda()
+    q, k, v = (normal(g, 3, H, dh, dtype="bf16") for _ in range(3))
+    gam = torch.linspace(0.5, 1.0, H)
+    o = torch.empty(3, H, dh, dtype=torch.bfloat16, device="cuda")
+    LinearAttentionDecoder(3, slots, H, dh).step(*(dev(x, "bf16") for x in (q, k, v)), gam.cuda(),
+                                                 i32(slot), pool, pool, o)
+    torch.cuda.synchronize()
+    for b, s in enumerate(slot):
+        w = ref.linear(q[b][None], k[b][None], v[b][None], gam.double(), [0, 1], dh ** -0.5, "bf16",
+                       S_in=S[b][None])
+        ref.within("o", o[b], w["o"])
+        ref.within("S", pool[s], w["S"])
+
+
+def test_two_streams_at_once(torch_cuda):
+    """Objects of their own on streams of their own: the same bits as in turn."""
+    from paper_2608_13578_amd import mixers
+    H, Hkv, dh, cu = 8, 2, 64, [0, 700, 1500, 1501, 2400]
+    g, total, n = rng(17), 2400, 4
+    q, do, k2, v2 = (dev(normal(g, total, H, dh, dtype="bf16"), "bf16") for _ in range(4))
+    k, v = (dev(normal(g, total, Hkv, dh, dtype="bf16"), "bf16") for _ in range(2))
+    gam, c = torch.linspace(0.8, 1.0, H, device="cuda"), i32(cu)
+
+    def make():
+        att, la = mixers.PackedAttention(total, n, H, Hkv, dh), mixers.LinearAttention(total, n, H, dh)
+        outs = [torch.empty_like(x) for x in (q, q, k, v, q, q, q, q)]
+        return att, la, outs, att.new_lse(), torch.empty(H, device="cuda")
+
+    def run(att, la, outs, lse, dg):
+        o, dq, dk, dv, y, eq, ek, ev = outs
+        att.forward(q, k, v, c, o, lse)
+        la.forward(q, k2, v2, gam, c, y)
+        att.backward(q, k, v, c, o, lse, do, dq, dk, dv)
+        la.backward(q, k2, v2, gam, c, do, eq, ek, ev, dgamma=dg)
+
+    sets = [make() for _ in range(3)]
+    run(*sets[0])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        for s, x in zip(streams, sets[1:]):
+            with torch.cuda.stream(s):
+                run(*x)
+    torch.cuda.synchronize()
+    for x in sets[1:]:
+        for a, b in zip(sets[0][2] + [sets[0][3], sets[0][4]], x[2] + [x[3], x[4]]):
+            assert torch.equal(a, b)
