@@ -476,7 +476,8 @@ int bcmt_attn_decode(const bcmt_attn_decode_config* cfg, const void* q, const vo
  * cut into pieces runs piece by piece on the states; an empty sequence passes its
  * state on.  gamma: H float32 on the device (0^0 is taken as 1), 4-byte aligned;
  * values outside [0, 1] give undefined numbers.
- * A value that is not finite reaches only its own row and later ones. */
+ * A value that is not finite reaches only its own row and later ones in the forward
+ * pass; in the backward pass it may reach every gradient of its sequence. */
 typedef struct {
   int32_t total, nseq, H, dh, dtype;
   float scale; /* finite */
