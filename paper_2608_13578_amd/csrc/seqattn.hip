@@ -81,7 +81,9 @@ struct PairLoads {
 // waves over 128 queries, two workgroups per CU and double buffers left a CU
 // waiting for its keys more than half of the time (16384 rows, 16 heads of 128:
 // 866 us, 471 us with the loads left out); eight waves halve the traffic, and
-// three tiles ahead hide the rest.
+// three tiles ahead hide the rest (462 us, 0.86 PFLOP/s).  Where few workgroups
+// make a launch, NG = 2 teams of NW waves take the tiles in turn, each through its own
+// ring, and are joined in LDS at the end.
 //
 // The maximum is raised only when a score passes it by more than 2^kRaise: the
 // weights then stay below 2^kRaise (their relative rounding is the same at any
@@ -91,26 +93,35 @@ struct PairLoads {
 
 constexpr float kRaise = 8.f;
 
-template <typename T, int DH, int NW_> struct QueryShape {
-  static constexpr int NW = NW_, NQ = sizeof(T) == 2 ? 2 : 1;
-  // buffers of the ring: 128 KB of LDS a workgroup, or 64 KB for two of four waves
-  static constexpr int NS = sizeof(T) == 2 ? (DH == 128 && NW == 4 ? 2 : 4) : DH == 128 ? 2 : 3;
-  static constexpr int WAVES = sizeof(T) == 4 ? 1 : 2;  // of a SIMD
+template <typename T, int DH, int NW_, int NG_> struct QueryShape {
+  static constexpr int NW = NW_, NG = NG_, NQ = sizeof(T) == 2 ? 2 : 1;
+  // buffers of a team's ring: 128 KB of LDS a workgroup, or 64 KB for two of four waves
+  static constexpr int NS = sizeof(T) == 2 ? (DH == 128 && NW == 4 ? 2 : 4)
+                            : DH == 128 || (DH == 64 && NG == 2) ? 2 : 3;
+  static constexpr int WAVES = sizeof(T) == 4 && NG == 1 ? 1 : 2;  // of a SIMD
 };
 
-template <typename T, int DH, int NW>
-__global__ __launch_bounds__(NW * 64, (QueryShape<T, DH, NW>::WAVES)) void seq_fwd_kernel(
+// The second team's part of a row joins the first's: what a wave leaves in LDS.
+template <int NQ, int NJ> struct TeamPart {
+  f32x4 a[NQ][NJ][64];
+  float m[NQ][64], l[NQ][64];
+  int dropped;
+};
+
+template <typename T, int DH, int NW, int NG>
+__global__ __launch_bounds__(NW * NG * 64, (QueryShape<T, DH, NW, NG>::WAVES)) void seq_fwd_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const int* __restrict__ cu, T* __restrict__ o, float* __restrict__ lse, int total, int nseq,
     int H, int G, int wph, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float sl2) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
-  constexpr int NQ = QueryShape<T, DH, NW>::NQ, NS = QueryShape<T, DH, NW>::NS;
+  constexpr int NQ = QueryShape<T, DH, NW, NG>::NQ, NS = QueryShape<T, DH, NW, NG>::NS;
   constexpr int KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
   constexpr int NI = kPairLoads<T, DH, NW>;
   constexpr int KUS = sizeof(T) == 2 ? 2 : 1;  // key groups read at once
-  __shared__ __attribute__((aligned(1024))) T lds[NS][2][64 * DH];
-  const int lane = threadIdx.x & 63, wave = wave_index();
+  __shared__ __attribute__((aligned(1024))) T ring[NG][NS][2][64 * DH];
+  const int lane = threadIdx.x & 63, wave = wave_index() % NW, team = wave_index() / NW;
+  T(*lds)[2][64 * DH] = ring[team];
   const int lr = lane & 15, lg = lane >> 4;
   const int QT = wph * 16 * NQ, hp = NW / wph, HG = H / hp;
   const int wq = wave % wph;
@@ -127,7 +138,7 @@ __global__ __launch_bounds__(NW * 64, (QueryShape<T, DH, NW>::WAVES)) void seq_f
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) tq[nq] = q0 + 16 * (nq & 1 ? 2 * wph - 1 - wq : wq);
   const int kend = min(be, q0 + QT);
-  const int nt = (kend - bs + 63) / 64;
+  const int nt = (kend - bs + 63) / 64, own = (nt - team + NG - 1) / NG;  // tiles; the team's
 
   F qf[NQ][KS];
 #pragma unroll
@@ -255,28 +266,57 @@ __global__ __launch_bounds__(NW * 64, (QueryShape<T, DH, NW>::WAVES)) void seq_f
 
   const PairLoads<T, DH, NW, (DH <= 64)> load(ldk, ldv, wave, lane);
   auto issue = [&](int it, int buf) __attribute__((always_inline)) {
-    load(kb, vb, bs + it * 64, kend - 1, lds[buf][0], lds[buf][1]);
+    load(kb, vb, bs + (it * NG + team) * 64, kend - 1, lds[buf][0], lds[buf][1]);
   };
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
-    if (i < nt) issue(i, i);
+    if (i < own) issue(i, i);
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
     for (int ds = 0; ds < KS; ++ds) settle(qf[nq][ds]);
   int buf = 0, next = NS - 1;
-  for (int it = 0; it < nt; ++it) {
-    if (it + NS - 2 < nt) vm_wait<(NS - 2) * NI>();
+  for (int it = 0; it * NG < nt; ++it) {
+    if (it + NS - 2 < own) vm_wait<(NS - 2) * NI>();
     else vm_wait<0>();
     wg_barrier();  // tile it is there, and every wave is done with the one before
-    if (it + NS - 1 < nt) issue(it + NS - 1, next);
-    const int kt = bs + it * 64;
+    if (it + NS - 1 < own) issue(it + NS - 1, next);
+    const int kt = bs + (it * NG + team) * 64;
     if (kt + 63 <= tq[0]) tile(std::false_type{}, kt, buf);
     else if (kt <= min(tq[NQ - 1] + 15, be - 1)) tile(std::true_type{}, kt, buf);
     buf = buf + 1 == NS ? 0 : buf + 1;
     next = next + 1 == NS ? 0 : next + 1;
   }
 
+  if constexpr (NG == 2) {
+    typedef TeamPart<NQ, NJ> Part;
+    static_assert(sizeof(Part) * NW <= sizeof(ring), "the parts lie in the ring");
+    Part* part = (Part*)&ring[0][0][0][0] + wave;
+    wg_barrier();  // every wave is done with its last tile
+    if (team == 1) {
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) part->a[nq][jj][lane] = oa[nq][jj];
+        part->m[nq][lane] = m[nq];
+        part->l[nq][lane] = l[nq];
+      }
+      if (lane == 0) part->dropped = dropped;
+    }
+    __syncthreads();
+    if (team == 1) return;
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+      const float mo = part->m[nq][lane], mn = fmaxf(m[nq], mo);
+      const float ms = mn == -INFINITY ? 0.f : mn;
+      const float w0 = exp2_fast(m[nq] - ms), w1 = exp2_fast(mo - ms);
+      l[nq] = l[nq] * w0 + part->l[nq][lane] * w1;
+      m[nq] = mn;
+#pragma unroll
+      for (int jj = 0; jj < NJ; ++jj) oa[nq][jj] = oa[nq][jj] * w0 + part->a[nq][jj][lane] * w1;
+    }
+    dropped = min(dropped, part->dropped);
+  }
   for (int u = dropped; u < min(be, tq[NQ - 1] + 16); ++u)  // (none, as a rule)
 #pragma unroll
     for (int jj = 0; jj < NJ; ++jj) {
@@ -307,17 +347,20 @@ __global__ __launch_bounds__(NW * 64, (QueryShape<T, DH, NW>::WAVES)) void seq_f
 
 // ------------------------------------------------------------------ backward: dQ
 // The forward's walk again, with delta_t = do_t . o_t formed (and stored for
-// dK/dV) first: s and dp per key tile, dz in place, dQ^T += K^T dZ^T.
+// dK/dV) first: s and dp per key tile, dz in place, dQ^T += K^T dZ^T.  The teams'
+// parts are added.  dz is rounded to the type as an operand: with the rounding of dq
+// itself an error of 2.5e-3 in the 2-norm in bfloat16 against 1.7e-3 of the output's
+// rounding alone; a second part of dz would add a third to the products.
 
 // Four waves a workgroup and one a SIMD for 128-wide heads: two would spill.
-template <typename T, int DH, int NW> struct DqShape {
+template <typename T, int DH, int NW, int NG> struct DqShape {
   static constexpr bool WIDE = sizeof(T) == 2 && DH == 128;
-  static constexpr int NS = WIDE ? 4 : QueryShape<T, DH, NW>::NS;
-  static constexpr int WAVES = WIDE ? 1 : QueryShape<T, DH, NW>::WAVES;
+  static constexpr int NS = WIDE ? 4 : QueryShape<T, DH, NW, NG>::NS;
+  static constexpr int WAVES = WIDE ? 1 : QueryShape<T, DH, NW, NG>::WAVES;
 };
 
-template <typename T, int DH, int NW>
-__global__ __launch_bounds__(NW * 64, (DqShape<T, DH, NW>::WAVES)) void seq_dq_kernel(
+template <typename T, int DH, int NW, int NG>
+__global__ __launch_bounds__(NW * NG * 64, (DqShape<T, DH, NW, NG>::WAVES)) void seq_dq_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const int* __restrict__ cu, const T* __restrict__ o, const float* __restrict__ lse,
     const T* __restrict__ dout, T* __restrict__ dq, float* __restrict__ delta, int total, int nseq,
@@ -325,12 +368,13 @@ __global__ __launch_bounds__(NW * 64, (DqShape<T, DH, NW>::WAVES)) void seq_dq_k
     float scale) {
   typedef typename Frag<T>::type F;
   typedef Tile<T, DH> TL;
-  constexpr int NQ = QueryShape<T, DH, NW>::NQ, NS = DqShape<T, DH, NW>::NS;
+  constexpr int NQ = QueryShape<T, DH, NW, NG>::NQ, NS = DqShape<T, DH, NW, NG>::NS;
   constexpr int KS = DH >= 32 ? DH / 32 : 1, NJ = DH / 16;
   constexpr int NI = kPairLoads<T, DH, NW>;
   constexpr int JB = NJ > 4 ? 4 : NJ;  // column operands read at once
-  __shared__ __attribute__((aligned(1024))) T lds[NS][2][64 * DH];
-  const int lane = threadIdx.x & 63, wave = wave_index();
+  __shared__ __attribute__((aligned(1024))) T ring[NG][NS][2][64 * DH];
+  const int lane = threadIdx.x & 63, wave = wave_index() % NW, team = wave_index() / NW;
+  T(*lds)[2][64 * DH] = ring[team];
   const int lr = lane & 15, lg = lane >> 4;
   const int QT = wph * 16 * NQ, hp = NW / wph, HG = H / hp;
   const int wq = wave % wph;
@@ -345,10 +389,10 @@ __global__ __launch_bounds__(NW * 64, (DqShape<T, DH, NW>::WAVES)) void seq_dq_k
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) tq[nq] = q0 + 16 * (nq & 1 ? 2 * wph - 1 - wq : wq);
   const int kend = min(be, q0 + QT);
-  const int nt = (kend - bs + 63) / 64;
+  const int nt = (kend - bs + 63) / 64, own = (nt - team + NG - 1) / NG;  // tiles; the team's
   const PairLoads<T, DH, NW, true> load(ldk, ldv, wave, lane);
   auto issue = [&](int it, int buf) __attribute__((always_inline)) {
-    load(kb, vb, bs + it * 64, kend - 1, lds[buf][0], lds[buf][1]);
+    load(kb, vb, bs + (it * NG + team) * 64, kend - 1, lds[buf][0], lds[buf][1]);
   };
 
   F qf[NQ][KS], df[NQ][KS];
@@ -369,7 +413,7 @@ __global__ __launch_bounds__(NW * 64, (DqShape<T, DH, NW>::WAVES)) void seq_dq_k
     part += __shfl_xor(part, 32, 64);
     dl[nq] = part;
     ls[nq] = t < be ? lse[(int64_t)h * total + t] * kLog2e : 0.f;
-    if (t < be && lg == 0) delta[(int64_t)h * total + t] = part;
+    if (team == 0 && t < be && lg == 0) delta[(int64_t)h * total + t] = part;
   }
   f32x4 da[NQ][NJ];
 #pragma unroll
@@ -442,7 +486,7 @@ __global__ __launch_bounds__(NW * 64, (DqShape<T, DH, NW>::WAVES)) void seq_dq_k
 
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
-    if (i < nt) issue(i, i);
+    if (i < own) issue(i, i);
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
     settle(ls[nq]);
@@ -453,16 +497,34 @@ __global__ __launch_bounds__(NW * 64, (DqShape<T, DH, NW>::WAVES)) void seq_dq_k
     }
   }
   int buf = 0, next = NS - 1;
-  for (int it = 0; it < nt; ++it) {
-    if (it + NS - 2 < nt) vm_wait<(NS - 2) * NI>();
+  for (int it = 0; it * NG < nt; ++it) {
+    if (it + NS - 2 < own) vm_wait<(NS - 2) * NI>();
     else vm_wait<0>();
     wg_barrier();  // tile it is there, and every wave is done with the one before
-    if (it + NS - 1 < nt) issue(it + NS - 1, next);
-    const int kt = bs + it * 64;
+    if (it + NS - 1 < own) issue(it + NS - 1, next);
+    const int kt = bs + (it * NG + team) * 64;
     if (kt + 63 <= tq[0]) tile(std::false_type{}, kt, buf);
     else if (kt <= min(tq[NQ - 1] + 15, be - 1)) tile(std::true_type{}, kt, buf);
     buf = buf + 1 == NS ? 0 : buf + 1;
     next = next + 1 == NS ? 0 : next + 1;
+  }
+  if constexpr (NG == 2) {
+    typedef f32x4 Part[NQ][NJ][64];
+    static_assert(sizeof(Part) * NW <= sizeof(ring), "the parts lie in the ring");
+    Part* part = (Part*)&ring[0][0][0][0] + wave;
+    wg_barrier();  // every wave is done with its last tile
+    if (team == 1) {
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) (*part)[nq][jj][lane] = da[nq][jj];
+    }
+    __syncthreads();
+    if (team == 1) return;
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+      for (int jj = 0; jj < NJ; ++jj) da[nq][jj] += (*part)[nq][jj][lane];
   }
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
@@ -741,31 +803,59 @@ bool wide_queries(DType dt, const SeqAttn& a) {
   return dt == DType::BF16 && query_grid(8, 2, a) >= 1024;
 }
 
-template <typename T, int DH, int NW>
+template <typename T, int DH, int NW, int NG = 1>
 hipError_t fwd_nw(const SeqAttn& a, hipStream_t s) {
-  const int64_t grid = query_grid(NW, QueryShape<T, DH, NW>::NQ, a);
+  const int64_t grid = query_grid(NW, QueryShape<T, DH, NW, NG>::NQ, a);
   const int G = a.H / a.Hkv;
-  seq_fwd_kernel<T, DH, NW><<<dim3((unsigned)grid), NW * 64, 0, s>>>(
+  seq_fwd_kernel<T, DH, NW, NG><<<dim3((unsigned)grid), NW * NG * 64, 0, s>>>(
       (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, (T*)a.o, a.lse, a.total, a.nseq, a.H, G,
       waves_per_head(NW, G), a.ldq, a.ldk, a.ldv, a.ldo, a.scale * kLog2e);
   return hipGetLastError();
 }
-template <typename T, int DH, int NW>
+template <typename T, int DH, int NW, int NG = 1>
 hipError_t dq_nw(const SeqAttn& a, hipStream_t s) {
-  const int64_t grid = query_grid(NW, QueryShape<T, DH, NW>::NQ, a);
+  const int64_t grid = query_grid(NW, QueryShape<T, DH, NW, NG>::NQ, a);
   const int G = a.H / a.Hkv;
-  seq_dq_kernel<T, DH, NW><<<dim3((unsigned)grid), NW * 64, 0, s>>>(
+  seq_dq_kernel<T, DH, NW, NG><<<dim3((unsigned)grid), NW * NG * 64, 0, s>>>(
       (const T*)a.q, (const T*)a.k, (const T*)a.v, a.cu, (const T*)a.o, a.lse, (const T*)a.dout,
       (T*)a.dq, a.delta, a.total, a.nseq, a.H, G, waves_per_head(NW, G), a.ldq, a.ldk, a.ldv, a.ldo,
       a.scale * kLog2e, a.scale);
   return hipGetLastError();
 }
 
+// Two teams of waves, which take the tiles of keys in turn and are joined at the end,
+// where the workgroups of one team are no more than two for a CU: half as many tiles
+// one after another, no fewer waves on a CU.  One sequence of 4096, 8 heads of 64 in
+// bfloat16 (256 workgroups): forward 55 us, 73 with one team, the whole gradient 148
+// and 170; 16 heads of 128 on 2 (512): forward 99 and 122; two of 3000, 12 heads of 64
+// (552): 65 and 58, 180 and 169.  Float32 heads of 64, whose tiles leave a CU room for
+// one workgroup only, take them always: eight sequences of 2048, 12 heads: 544 and 621
+// us, 1853 and 1912 (of 32: 629 and 512).  Sequences of one tile have nothing to share.
+template <typename T, int DH>
+bool two_teams(const SeqAttn& a) {
+  constexpr int NQ = sizeof(T) == 2 ? 2 : 1;
+  const int wph = waves_per_head(4, a.H / a.Hkv);
+  const int64_t grid = (int64_t)(a.total / (wph * 16 * NQ)) * (a.H * wph / 4);
+  return a.total > 64 * (int64_t)a.nseq && (grid <= 512 || (sizeof(T) == 4 && DH == 64));
+}
+
 template <typename T, int DH>
 hipError_t fwd_t(const SeqAttn& a, hipStream_t s) {
   if constexpr (sizeof(T) == 2)
     if (wide_queries(DType::BF16, a)) return fwd_nw<T, DH, 8>(a, s);
+  if constexpr (sizeof(T) * DH <= 256)  // (float32 heads of 128: their LDS is full)
+    if (two_teams<T, DH>(a)) return fwd_nw<T, DH, 4, 2>(a, s);
   return fwd_nw<T, DH, 4>(a, s);
+}
+
+template <typename T, int DH>
+hipError_t dq_t(const SeqAttn& a, hipStream_t s) {
+  if constexpr (DH <= 64) {
+    if constexpr (sizeof(T) == 2)
+      if (wide_queries(DType::BF16, a)) return dq_nw<T, DH, 8>(a, s);
+    if (two_teams<T, DH>(a)) return dq_nw<T, DH, 4, 2>(a, s);
+  }
+  return dq_nw<T, DH, 4>(a, s);
 }
 
 // Parts of a group's heads for dK and dV: a divisor of G, until there are two
@@ -785,11 +875,7 @@ int parts_t(int total, int nseq, int Hkv, int G) {
 template <typename T, int DH>
 hipError_t bwd_t(const SeqAttn& a, hipStream_t s) {
   const int G = a.H / a.Hkv;
-  hipError_t e;
-  if constexpr (sizeof(T) == 2 && DH <= 64)
-    e = wide_queries(DType::BF16, a) ? dq_nw<T, DH, 8>(a, s) : dq_nw<T, DH, 4>(a, s);
-  else
-    e = dq_nw<T, DH, 4>(a, s);
+  hipError_t e = dq_t<T, DH>(a, s);
   if (e != hipSuccess) return e;
   constexpr int KT = 64 * KeyShape<T, DH>::NK;
   const int parts = parts_t<T, DH>(a.total, a.nseq, a.Hkv, G);

@@ -858,3 +858,26 @@ def test_two_streams_at_once(torch_cuda):
     for x in sets[1:]:
         for a, b in zip(sets[0][2] + [sets[0][3], sets[0][4]], x[2] + [x[3], x[4]]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("f32", 16), ("bf16", 128), ("f32", 128)])
+def test_attention_of_short_sequences_with_values_that_are_not_finite(torch_cuda, dtype, dh):
+    """As above, where one team of waves takes all keys of a workgroup's queries."""
+    from paper_2608_13578_amd.mixers import PackedAttention
+    lens = [150] + [30] * 20
+    cu, total, q, k, v, do = attn_inputs((dtype, dh, 2, 1, lens, 0, 0, False, 1.0), 18)
+    want = ref.attention(q, k, v, cu, dh ** -0.5, dtype)
+    qd, kd, vd = (dev(x, dtype) for x in (q, k, v))
+    vd[100, 0, 5] = -math.inf
+    vd[cu[3] + 7] = math.nan
+    att = PackedAttention(total, len(lens), 2, 1, dh, dtype)
+    o = torch.zeros_like(qd)
+    att.forward(qd, kd, vd, i32(cu), o)
+    torch.cuda.synchronize()
+    hit = list(range(cu[3] + 7, cu[4]))
+    clean = [t for t in range(total) if t not in hit and not 100 <= t < 150]
+    ref.within("o", o, want["o"], clean)
+    assert not bool(torch.isfinite(o[hit].float()).any())
+    assert bool((o[100:150, :, 5] == -math.inf).all())
+    rest = [c for c in range(dh) if c != 5]
+    ref.within("o", o[100:150][:, :, rest], tuple(x[100:150][:, :, rest] for x in want["o"]))
