@@ -94,10 +94,11 @@ int check_decode(const bcmt_attn_decode_config* c) {
   if (c->cs || c->ct || c->ch) {
     for (int64_t s : {c->cs, c->ct, c->ch})
       if (s < c->dh || s % (16 / es) != 0) return BCMT_ERR_INVALID;
-    // the caches' extent in bytes fits 62 bits
-    if ((double)c->slots * c->cs + (double)c->cap * c->ct + (double)c->Hkv * c->ch > 1e18)
-      return BCMT_ERR_INVALID;
   }
+  // the caches' extent in bytes fits 62 bits
+  const double cs = c->cs ? (double)c->cs : (double)c->cap * wk;
+  if (c->slots * cs + (double)c->cap * c->ct + (double)c->Hkv * c->ch > 1e18)
+    return BCMT_ERR_INVALID;
   if (st != BCMT_OK) return st;
   const int nh = (c->H / c->Hkv + 15) / 16;
   if (c->cap > kMaxTotal || c->slots > kMaxTotal || (int64_t)c->B * c->Hkv * nh > 65535 || c->H > 65535)

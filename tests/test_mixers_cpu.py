@@ -188,3 +188,9 @@ def test_columns_of_one_array_do_not_meet():
     # the last head of a row must not reach into the next row's first column
     cols = dict(dq=base, dk=base + 2 * 8 * 64, dv=base + 2 * 11 * 64)
     assert call("bcmt_attn_backward", cfg, AB, ws_bytes=0, **cols) == INVALID
+
+
+def test_dense_caches_past_62_bits():
+    assert abi.bcmt_attn_decode_validate(dec(slots=1 << 30, cap=1 << 30)) == INVALID
+    assert abi.bcmt_attn_decode_workspace_bytes(dec(slots=1 << 30, cap=1 << 30)) == 0
+    assert abi.bcmt_attn_decode_validate(dec(slots=1 << 20, cap=1 << 20)) == abi.BCMT_OK
