@@ -98,13 +98,11 @@ struct Tile {
   }
   // The same loads of whole tiles with the lane's part of the address formed once
   // (lane_off: bytes from the tile's lowest row, whose address is the wave's): one
-  // vector instruction a load instead of ten.  `down`: row r of the tile is r rows
-  // below its first.  Row strides up to kNearLd, so that a tile's rows are within
-  // 2^32 bytes.
-  __device__ static __forceinline__ unsigned lane_off(int64_t ld, bool down, int i, int lane) {
+  // vector instruction a load instead of ten.  Row strides up to kNearLd, so that a
+  // tile's rows are within 2^32 bytes.
+  __device__ static __forceinline__ unsigned lane_off(int64_t ld, int i, int lane) {
     const int id = i * 64 + lane, row = id / NCH, pos = id % NCH;
-    return (unsigned)((down ? 63 - row : row) * (unsigned)ld + (pos ^ swz(row)) * CH) *
-           (unsigned)sizeof(T);
+    return (unsigned)(row * (unsigned)ld + (pos ^ swz(row)) * CH) * (unsigned)sizeof(T);
   }
   __device__ static __forceinline__ void issue_near(const T* lowest, unsigned off, T* t, int i) {
     __builtin_amdgcn_global_load_lds((const char*)lowest + off, (lds_void_t*)(t + i * 64 * CH), 16, 0,
@@ -265,7 +263,7 @@ __device__ __forceinline__ SeqTile find_item(const int* __restrict__ cu, int nse
     end = min(max(cu[lane + 1], begin), total);
   }
   const int n = (end - begin + TILE - 1) / TILE;
-  auto f = [&](int t) {  // (at most total / TILE + 64 tiles: exact in float32 up to 2^24)
+  auto f = [&](int t) {  // (at most total / TILE + 64 tiles, below 2^24: exact in float32)
     return (int)wave_sum((float)max(0, n - t));
   };
   int lo = 0, hi = (total + TILE - 1) / TILE;  // f(hi) = 0
@@ -284,7 +282,7 @@ __device__ __forceinline__ SeqTile find_item(const int* __restrict__ cu, int nse
   }
   const unsigned long long has = __ballot(n > lo);
   const bool mine = n > lo && (int)__popcll(has & ((1ull << lane) - 1)) == x - fhi;
-  const int s = __builtin_ctzll(__ballot(mine));
+  const int s = __builtin_ctzll(__ballot(mine) | 1ull << 63);  // (none: offsets out of order)
   r.seq = s;
   r.begin = __builtin_amdgcn_readlane(begin, s);
   r.end = __builtin_amdgcn_readlane(end, s);

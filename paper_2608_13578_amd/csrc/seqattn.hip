@@ -51,7 +51,7 @@ struct PairLoads {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int gi = wave * NI + i;
-      off[i] = TL::lane_off(gi < TL::NCH ? lda : ldb, false, gi % TL::NCH, lane);
+      off[i] = TL::lane_off(gi < TL::NCH ? lda : ldb, gi % TL::NCH, lane);
     }
   }
   // Rows r0 .. r0 + 63 of a and b (those behind rlast: rlast's) into ta and tb.
