@@ -1030,9 +1030,12 @@ hipError_t lin_step(DType dt, int dh, const LinStep& a, hipStream_t s) {
 
 // Rows of a segment: such that the workgroups, at most total / seg + nseq of a group
 // of heads, are one round of those that the chip holds at once (one of eight waves
-// to a CU), or, with many sequences, a quarter of it more than these.  At least 256
-// rows: a boundary's state, written twice and read twice, costs the traffic of a few
-// chunks.
+// to a CU), or, with many sequences, a quarter of it more than these (131072 rows, 16
+// heads of 64, by segments of 1024, 4544 and 8192 rows: sums 117, 131, 173 us, operator
+// 270, 266, 373, scan 22, 7, 5).  Down to one chunk: where that leaves CUs idle, the
+// chunks of a segment one after another are the time (1024 rows of 12 heads of 64,
+// forward and gradients, at least 64, 128 or 256 rows: 62, 67, 93 us; of 8 float32
+// heads of 128: 176, 246, 405).
 int lin_segment_rows(DType dt, int total, int nseq, int H, int dh) {
   const int row = dh * (dt == DType::BF16 ? 2 : 4), hp = row < 256 ? 256 / row : 1;
   const int round = 256 / ((H + hp - 1) / hp);  // segments of a group of heads
@@ -1040,7 +1043,7 @@ int lin_segment_rows(DType dt, int total, int nseq, int H, int dh) {
   if (n < round / 4) n = round / 4;
   if (n < 1) n = 1;
   const int64_t want = ((int64_t)total + n - 1) / n;
-  return (int)(want < 256 ? 256 : (want + kC - 1) / kC * kC);
+  return (int)((want + kC - 1) / kC * kC);
 }
 
 }  // namespace bcmt

@@ -66,9 +66,10 @@ class _Mixer:
     def _call(self, fn, stream, *args):
         """Enqueues on the caller's stream, or the current one of this object's
         device, which is made the current device for the call."""
-        if stream is None:
-            stream = torch.cuda.current_stream(self._index)
-        s = stream if isinstance(stream, int) else stream.cuda_stream
+        if stream is None:  # (the address alone: 0.1 us, the stream object 1.1)
+            s = torch._C._cuda_getCurrentRawStream(self._index)
+        else:
+            s = stream if isinstance(stream, int) else stream.cuda_stream
         if torch.cuda.current_device() == self._index:
             st = fn(self._ref, *args, s)
         else:

@@ -328,7 +328,7 @@ LINEAR = [
 def test_linear_attention(torch_cuda, case):
     from paper_2608_13578_amd.mixers import LinearAttention
     dtype, dh, decays, lens, lead, behind, fused, states = case
-    say(f"linear attention {case}")
+    say(f"linear attention {dtype} {dh} {len(decays)} heads {lens}")
     H, cu, scale = len(decays), offsets(lens, lead), dh ** -0.5
     total = cu[-1] + behind
     g = rng(7)
@@ -881,3 +881,23 @@ def test_attention_of_short_sequences_with_values_that_are_not_finite(torch_cuda
     assert bool((o[100:150, :, 5] == -math.inf).all())
     rest = [c for c in range(dh) if c != 5]
     ref.within("o", o[100:150][:, :, rest], tuple(x[100:150][:, :, rest] for x in want["o"]))
+
+
+# Heads for the whole chip, so that a segment of a sequence holds several chunks.
+LINEAR_MANY = [
+    ("bf16", 64, 96, [500, 120], 0, 0, True, True),
+    ("bf16", 32, 193, [300, 70], 1, 0, False, True),
+    ("bf16", 16, 380, [300, 1, 70], 0, 2, False, False),
+    ("bf16", 128, 48, [400, 130], 0, 0, False, True),
+    ("f32", 64, 50, [500, 0, 120], 0, 0, False, True),
+    ("f32", 16, 190, [300, 70], 2, 1, True, True),
+    ("f32", 128, 48, [400, 130], 0, 0, False, False),
+    ("bf16", 64, 520, [150, 50], 0, 0, False, True),  # no sequence is cut
+    ("f32", 32, 520, [150, 50], 0, 0, False, True),
+]
+
+
+@pytest.mark.parametrize("case", LINEAR_MANY, ids=lambda c: f"{c[0]}-dh{c[1]}-H{c[2]}-{sum(c[3])}rows")
+def test_linear_attention_of_many_heads(torch_cuda, case):
+    dtype, dh, H, *rest = case
+    test_linear_attention(torch_cuda, (dtype, dh, [0.8 + 0.2 * i / (H - 1) for i in range(H)], *rest))
