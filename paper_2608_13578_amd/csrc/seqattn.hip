@@ -17,6 +17,7 @@
 // the second operand of the next product as they are (Tile::col8 reads the
 // first operand in the same key order).  dK/dV computes them untransposed,
 // one key per lane, to the same end.
+#include <algorithm>
 #include <climits>
 #include <type_traits>
 
@@ -545,8 +546,8 @@ __global__ __launch_bounds__(NW * NG * 64, (DqShape<T, DH, NW, NG>::WAVES)) void
 // waves take the steps in turn and are joined at the end, so that a SIMD has
 // two waves and the keys with the most queries behind them are done sooner.
 // Shared heads are summed in registers, in a fixed order; where there are too
-// few workgroups for the chip, each takes a part of the group's heads and leaves
-// float32 sums that a second kernel adds.
+// few workgroups for the chip, several take the steps of the same keys in turn
+// and leave float32 sums that a second kernel adds.
 
 template <typename T, int DH> struct KeyShape {
   static constexpr int NK = sizeof(T) == 2 ? 2 : 1;  // groups of 16 keys of a wave
@@ -578,9 +579,8 @@ __global__ __launch_bounds__((KeyShape<T, DH>::NH * 256)) void seq_dkdv_kernel(
   const SeqTile st = find_item<true>(cu, nseq, total, KT, (int)(blockIdx.x / (Hkv * parts)));
   const int be = st.end, k0 = st.begin + st.tile * KT;
   if (st.tile < 0 || k0 >= be) return;
-  const int heads = G / parts, h0 = j * G + pt * heads;
-  const int nt1 = (be - k0 + 63) / 64, nstep = nt1 * heads;  // query tiles of a head, of all
-  const int nt = (nstep + NH - 1) / NH;
+  const int nt1 = (be - k0 + 63) / 64, nstep = nt1 * G;  // query tiles of a head, of all
+  const int nt = (nstep + NH * (parts - pt) - 1) / (NH * parts);  // rounds of this part's teams
 
   int uk[NK];
   F kf[NK][KS], vf[NK][KS];
@@ -602,10 +602,10 @@ __global__ __launch_bounds__((KeyShape<T, DH>::NH * 256)) void seq_dkdv_kernel(
   }
   constexpr int TILE = 64 * DH;
   const PairLoads<T, DH, NW, (DH <= 32)> load(ldq, ldo, wave, lane);
-  // step it NH + team into a buffer (beyond the last step: the last one again)
+  // the team's step of a round into a buffer (beyond the last step: the last one again)
   auto issue = [&](int it, int buf) __attribute__((always_inline)) {
-    const int step = min(it * NH + team, nstep - 1);
-    const int h = h0 + step / nt1, tt = k0 + (step % nt1) * 64;
+    const int step = min((it * parts + pt) * NH + team, nstep - 1);
+    const int h = j * G + step / nt1, tt = k0 + (step % nt1) * 64;
     T* t = lds + (buf * NH + team) * 2 * TILE;
     load(q + h * DH, dout + h * DH, tt, be - 1, t, t + TILE);
     const float* src = (wave & 1 ? delta : lse) + (int64_t)h * total + min(tt + lane, be - 1);
@@ -707,9 +707,9 @@ __global__ __launch_bounds__((KeyShape<T, DH>::NH * 256)) void seq_dkdv_kernel(
   for (int it = 0; it < nt; ++it) {
     if (it + NS - 2 < nt) vm_wait<(NS - 2) * NI>();
     else vm_wait<0>();
-    wg_barrier();  // the steps it NH .. are there, and every wave is done with those before
+    wg_barrier();  // the round's steps are there, and every wave is done with those before
     if (it + NS - 1 < nt) issue(it + NS - 1, next);
-    const int step = it * NH + team, tt = k0 + (step % nt1) * 64;
+    const int step = (it * parts + pt) * NH + team, tt = k0 + (step % nt1) * 64;
     if (step < nstep && uk[0] < be) {
       if (tt >= uk[NK - 1] + 15 && tt + 64 <= be) tile(std::false_type{}, tt, buf);
       else if (tt + 63 >= uk[0]) tile(std::true_type{}, tt, buf);
@@ -858,18 +858,20 @@ hipError_t dq_t(const SeqAttn& a, hipStream_t s) {
   return dq_nw<T, DH, 4>(a, s);
 }
 
-// Parts of a group's heads for dK and dV: a divisor of G, until there are two
-// workgroups for every CU (the whole gradient of four sequences of 2048, 16 heads of
-// 64 on 4: 196 us, 213 with four, 244 with one, 247 with no parts; of one sequence of
-// 4096, 16 heads of 128 on 2: 401, 403, 574 and 1747).
-int head_parts(int64_t tiles, int Hkv, int G) {
-  int p = 1;
-  while (p < G && (G % p || tiles * Hkv * p < 512)) ++p;
-  return p;
-}
+// Parts of the steps for dK and dV, until there are two workgroups for every CU (the
+// whole gradient of four sequences of 2048, 16 heads of 64 on 4: 179 us, 200 with
+// four, 244 with no parts; of one of 4096, 16 heads of 128 on 2: 405, the same, 1747).
+// As many as the group has heads; more, up to 16, while a part has 8 rounds of its
+// teams (float32: 4, which take longer): a part costs the traffic of its float32 sums
+// (one sequence of 4096, 8 heads of 64 in bfloat16: 131 us with two parts, 146 with
+// one; two of 1024: 55 with four and 48 with one).
 template <typename T, int DH>
 int parts_t(int total, int nseq, int Hkv, int G) {
-  return head_parts(total / (64 * KeyShape<T, DH>::NK) + nseq, Hkv, G);
+  typedef KeyShape<T, DH> KS;
+  const int64_t wgs = ((int64_t)total / (64 * KS::NK) + nseq) * Hkv;
+  const int64_t rounds = (int64_t)total * G / ((int64_t)64 * nseq * KS::NH);
+  const int64_t most = std::max<int64_t>(G, std::min<int64_t>(rounds / (sizeof(T) == 2 ? 8 : 4), 16));
+  return (int)std::min((512 + wgs - 1) / wgs, most);
 }
 
 template <typename T, int DH>

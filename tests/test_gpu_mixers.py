@@ -901,3 +901,18 @@ LINEAR_MANY = [
 def test_linear_attention_of_many_heads(torch_cuda, case):
     dtype, dh, H, *rest = case
     test_linear_attention(torch_cuda, (dtype, dh, [0.8 + 0.2 * i / (H - 1) for i in range(H)], *rest))
+
+
+# Long sequences of few heads: several workgroups take the queries of the same keys.
+ATTN_LONG = [
+    ("bf16", 64, 1, 1, [2117], 0, 3, False, 1.0),
+    ("bf16", 128, 2, 2, [1201], 1, 0, True, 1.0),
+    ("bf16", 32, 3, 1, [1500, 1130], 0, 0, False, 1.0),
+    ("f32", 128, 1, 1, [1203], 0, 0, False, 1.0),
+    ("f32", 16, 2, 1, [1100], 2, 1, True, 1.0),
+]
+
+
+@pytest.mark.parametrize("case", ATTN_LONG, ids=lambda c: f"{c[0]}-dh{c[1]}-H{c[2]}.{c[3]}-{sum(c[4])}rows")
+def test_attention_of_long_sequences(torch_cuda, case):
+    test_attention(torch_cuda, case)
