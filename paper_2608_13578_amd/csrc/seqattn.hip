@@ -1180,10 +1180,14 @@ hipError_t seq_attn_decode(DType dt, int dh, const DecAttn& a, hipStream_t s) {
 // different lengths even out (32 of up to 8192 positions, 8 heads of 128: 111 us,
 // 119 with two or eight per CU; 32 of 4096 each: 106, 105 and 119), at least two
 // tiles of every wave in a part, and no more parts than CUs, since the join reads
-// them all (one sequence of 131072, one head: 23 us with 256, 32 with 512).
+// them all (one sequence of 131072, one head: 23 us with 256, 32 with 512).  Caches of
+// at most eight tiles a wave stay whole and need no second launch (12 heads of 64, one
+// and four parts: 512 positions 7.1 and 8.6 us, 1024 positions 9.7 and 8.6, but 11.6
+// and 14.4 called from a host; 32 sequences of up to 1024, 8 heads of 128: 18 and 29).
 int seq_attn_decode_splits(DType dt, int dh, int B, int H, int Hkv, int cap) {
   const int G = H / Hkv, NH = (G + 15) / 16;
   const int nw = (dt == DType::BF16 ? 2 : 4) * dh >= 512 ? 2 : 4;
+  if (cap <= nw * 256) return 1;
   const int64_t wgs = (int64_t)B * Hkv * NH;
   const int64_t want = wgs < 4 ? 256 : (1024 + wgs - 1) / wgs, most = (cap + nw * 64 - 1) / (nw * 64);
   const int64_t n = want < most ? want : most;
