@@ -395,7 +395,9 @@ int bcmt_model_train_step(const bcmt_model_config* cfg, const int32_t* tokens,
  *   o_t = sum_u p_tu v_u,  p_tu = exp(scale q_t.k_u - lse_t),
  *   lse_t = log sum_u exp(scale q_t.k_u)
  * Softmax statistics and sums are float32; in bf16 the weights p (and their
- * gradient) are rounded to bf16 as operands of the products.
+ * gradient) are rounded to bf16 as operands of the products, and the backward
+ * pass takes sum_u p_tu (dO_t.v_u) as dO_t.o_t of the rounded o: where a row's
+ * weights are nearly all on one key, its dq keeps that rounding's error.
  *
  *   - Rows hold heads side by side: row r of q is q + r ldq, head h at h dh.  A
  *     stride of 0 means dense rows (H dh or Hkv dh elements); otherwise it is
