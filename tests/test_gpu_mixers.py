@@ -919,3 +919,38 @@ ATTN_LONG = [
 @pytest.mark.parametrize("case", ATTN_LONG, ids=lambda c: f"{c[0]}-dh{c[1]}-H{c[2]}.{c[3]}-{sum(c[4])}rows")
 def test_attention_of_long_sequences(torch_cuda, case):
     test_attention(torch_cuda, case)
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("f32", 16), ("bf16", 128)])
+def test_gradients_of_offsets_out_of_order_stay_inside(torch_cuda, dtype, dh):
+    """Nothing outside the arrays is written, and correct offsets after it give
+    what they gave before."""
+    from paper_2608_13578_amd.mixers import LinearAttention, PackedAttention
+    total, H, n = 700, 4, 3
+    g = rng(19)
+    q, k, v, do = (dev(normal(g, total, H, dh, dtype=dtype), dtype) for _ in range(4))
+    k2, v2 = (x[:, :2].contiguous() for x in (k, v))
+    gam = torch.full((H,), 0.9, device="cuda")
+    att = PackedAttention(total, n, H, 2, dh, dtype)
+    la = LinearAttention(total, n, H, dh, dtype)
+    guards = [torch.full((total + 64, h, dh), 7.0, dtype=DT[dtype], device="cuda")
+              for h in (H, H, 2, 2, H, H, H)]
+    o, dq, dk, dv, eq, ek, ev = (x[:total] for x in guards)
+    lse, dg = torch.zeros(H, total, device="cuda"), torch.zeros(H, device="cuda")
+    S = la.new_state()
+
+    def run(cu):
+        c = i32(cu)
+        att.forward(q, k2, v2, c, o, lse)
+        att.backward(q, k2, v2, c, o, lse, do, dq, dk, dv)
+        la.backward(q, k, v, gam, c, do, eq, ek, ev, S, None, None, dg)
+        torch.cuda.synchronize()
+        return [x.clone() for x in (o, dq, dk, dv, eq, ek, ev, dg)]
+
+    first = run([0, 300, 301, 700])
+    for cu in ([0, 500, 50, 700], [0, 1 << 30, 5, -7], [-5, 200, 2000000000, 2147483647], [700, 0, 700, 0]):
+        run(cu)
+        for x in guards:
+            assert bool((x[total:] == 7.0).all())
+    for x, y in zip(first, run([0, 300, 301, 700])):
+        assert torch.equal(x, y)
