@@ -4,9 +4,13 @@
 Allocation and argument checks only: the arithmetic runs in the library's HIP
 kernels.  The C ABI takes bare pointers, so every tensor is checked here
 against the configuration: type, extent, row stride, contiguity and device.
-An object belongs to the device that it was made for and keeps one workspace:
-its calls must be ordered (one stream, or streams that wait for each other),
-and a captured graph replays in that workspace.
+An object belongs to the device that it was made for.  Where a call needs a
+workspace, the object keeps one for every stream that it is called on, allocated
+on that stream at the first such call: torch's allocator orders memory by the
+stream that it was allocated on, so neither an earlier nor a later owner of the
+memory can meet the kernels.  A captured graph replays in the workspace of the
+stream that it was captured on: graphs captured on one stream must not replay at
+the same time, and the object must outlive them.
 """
 
 import ctypes
@@ -31,8 +35,22 @@ class _Mixer:
         self._ref = ctypes.byref(cfg)
         self._lib = abi.lib()
 
-    def _scratch(self, n):
-        return torch.empty(max(256, n), dtype=torch.uint8, device=self.device)
+    def _stream(self, stream):
+        """The address of the caller's stream, or of the current one of this
+        object's device (the address alone: 0.1 us, the stream object 1.1)."""
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self._index)
+        return stream if isinstance(stream, int) else stream.cuda_stream
+
+    def _scratch(self, held, n, s):
+        """(address, bytes) of the workspace of stream s, kept in `held`."""
+        ws = held.get(s)
+        if ws is None:
+            on = torch.cuda.ExternalStream(s, device=self.device) if s else \
+                torch.cuda.default_stream(self.device)
+            with torch.cuda.stream(on):
+                ws = held[s] = torch.empty(max(256, n), dtype=torch.uint8, device=self.device)
+        return ws.data_ptr(), ws.numel()
 
     def _rows(self, name, t, rows, width, ld):
         """The address of a tensor of `rows` rows of `width` elements (in any
@@ -63,13 +81,8 @@ class _Mixer:
                              f"{self.device} is wanted")
         return t.data_ptr()
 
-    def _call(self, fn, stream, *args):
-        """Enqueues on the caller's stream, or the current one of this object's
-        device, which is made the current device for the call."""
-        if stream is None:  # (the address alone: 0.1 us, the stream object 1.1)
-            s = torch._C._cuda_getCurrentRawStream(self._index)
-        else:
-            s = stream if isinstance(stream, int) else stream.cuda_stream
+    def _call(self, fn, s, *args):
+        """Enqueues on stream s; this object's device is the current one for the call."""
         if torch.cuda.current_device() == self._index:
             st = fn(self._ref, *args, s)
         else:
@@ -87,7 +100,7 @@ class PackedAttention(_Mixer):
                  ldo=0, device="cuda"):
         self._setup(abi.make_attn_config(total, nseq, H, Hkv, dh, dtype, scale, ldq, ldk, ldv, ldo),
                     abi.bcmt_attn_validate, dtype, device)
-        self.ws = None
+        self._ws, self._ws_bytes = {}, abi.bcmt_attn_workspace_bytes(self.cfg)
         self._total, self._nseq, self._H = total, nseq, H
         self._wq, self._wk = H * dh, Hkv * dh
         self._ld = ldq, ldk, ldv, ldo
@@ -106,7 +119,7 @@ class PackedAttention(_Mixer):
         return torch.empty((self._H, self._total), dtype=torch.float32, device=self.device)
 
     def forward(self, q, k, v, cu, o, lse=None, stream=None):
-        self._call(self._lib.bcmt_attn_forward, stream, *self._inputs(q, k, v, cu),
+        self._call(self._lib.bcmt_attn_forward, self._stream(stream), *self._inputs(q, k, v, cu),
                    self._rows("o", o, self._total, self._wq, self._ld[3]),
                    self._array("lse", lse, (self._H, self._total), torch.float32, True))
 
@@ -116,9 +129,9 @@ class PackedAttention(_Mixer):
                 self._array("lse", lse, (self._H, n), torch.float32),
                 self._rows("dO", dO, n, wq, ldo), self._rows("dq", dq, n, wq, ldq),
                 self._rows("dk", dk, n, wk, ldk), self._rows("dv", dv, n, wk, ldv))
-        if self.ws is None:
-            self.ws = self._scratch(abi.bcmt_attn_workspace_bytes(self.cfg))
-        self._call(self._lib.bcmt_attn_backward, stream, *args, self.ws.data_ptr(), self.ws.numel())
+        s = self._stream(stream)
+        self._call(self._lib.bcmt_attn_backward, s, *args,
+                   *self._scratch(self._ws, self._ws_bytes, s))
 
 
 class AttentionDecoder(_Mixer):
@@ -130,7 +143,7 @@ class AttentionDecoder(_Mixer):
         self._setup(abi.make_attn_decode_config(B, slots, cap, H, Hkv, dh, dtype, scale, ldq, ldk,
                                                 ldv, ldo, cs, ct, ch),
                     abi.bcmt_attn_decode_validate, dtype, device)
-        self.ws = self._scratch(abi.bcmt_attn_decode_workspace_bytes(self.cfg))
+        self._ws, self._ws_bytes = {}, abi.bcmt_attn_decode_workspace_bytes(self.cfg)
         self._B, self._wq, self._wk = B, H * dh, Hkv * dh
         self._ld = ldq, ldk, ldv, ldo
         self._shape = (slots, cap, Hkv, dh)
@@ -153,12 +166,13 @@ class AttentionDecoder(_Mixer):
 
     def step(self, q, k, v, slot, length, kcache, vcache, o, stream=None):
         n, wq, wk, (ldq, ldk, ldv, ldo) = self._B, self._wq, self._wk, self._ld
-        self._call(self._lib.bcmt_attn_decode, stream, self._rows("q", q, n, wq, ldq),
+        s = self._stream(stream)
+        self._call(self._lib.bcmt_attn_decode, s, self._rows("q", q, n, wq, ldq),
                    self._rows("k", k, n, wk, ldk), self._rows("v", v, n, wk, ldv),
                    self._array("slot", slot, (n,), torch.int32, True),
                    self._array("length", length, (n,), torch.int32),
                    self._cache("kcache", kcache), self._cache("vcache", vcache),
-                   self._rows("o", o, n, wq, ldo), self.ws.data_ptr(), self.ws.numel())
+                   self._rows("o", o, n, wq, ldo), *self._scratch(self._ws, self._ws_bytes, s))
 
 
 class LinearAttention(_Mixer):
@@ -169,8 +183,10 @@ class LinearAttention(_Mixer):
                  device="cuda"):
         self._setup(abi.make_linattn_config(total, nseq, H, dh, dtype, scale, ldq, ldk, ldv, ldo),
                     abi.bcmt_linattn_validate, dtype, device)
-        self.ws = self._scratch(abi.bcmt_linattn_workspace_bytes(self.cfg, abi.BCMT_PASS_FORWARD))
-        self.ws_bwd = None
+        self._ws, self._ws_bwd = {}, {}
+        self._ws_bytes, self._ws_bwd_bytes = (
+            abi.bcmt_linattn_workspace_bytes(self.cfg, p)
+            for p in (abi.BCMT_PASS_FORWARD, abi.BCMT_PASS_BACKWARD))
         self._total, self._nseq, self._H, self._w = total, nseq, H, H * dh
         self._ld = ldq, ldk, ldv, ldo
         self._shape = (nseq, H, dh, dh)
@@ -190,9 +206,10 @@ class LinearAttention(_Mixer):
         return self._array(name, t, self._shape, torch.float32, True)
 
     def forward(self, q, k, v, gamma, cu, o, S_in=None, S_out=None, stream=None):
-        self._call(self._lib.bcmt_linattn_forward, stream, *self._inputs(q, k, v, gamma, cu),
+        s = self._stream(stream)
+        self._call(self._lib.bcmt_linattn_forward, s, *self._inputs(q, k, v, gamma, cu),
                    self._state("S_in", S_in), self._rows("o", o, self._total, self._w, self._ld[3]),
-                   self._state("S_out", S_out), self.ws.data_ptr(), self.ws.numel())
+                   self._state("S_out", S_out), *self._scratch(self._ws, self._ws_bytes, s))
 
     def backward(self, q, k, v, gamma, cu, dO, dq, dk, dv, S_in=None, dS_out=None, dS_in=None,
                  dgamma=None, stream=None):
@@ -202,11 +219,9 @@ class LinearAttention(_Mixer):
                 self._rows("dq", dq, n, w, ldq), self._rows("dk", dk, n, w, ldk),
                 self._rows("dv", dv, n, w, ldv), self._state("dS_in", dS_in),
                 self._array("dgamma", dgamma, (self._H,), torch.float32, True))
-        if self.ws_bwd is None:
-            self.ws_bwd = self._scratch(abi.bcmt_linattn_workspace_bytes(self.cfg,
-                                                                         abi.BCMT_PASS_BACKWARD))
-        self._call(self._lib.bcmt_linattn_backward, stream, *args, self.ws_bwd.data_ptr(),
-                   self.ws_bwd.numel())
+        s = self._stream(stream)
+        self._call(self._lib.bcmt_linattn_backward, s, *args,
+                   *self._scratch(self._ws_bwd, self._ws_bwd_bytes, s))
 
 
 class LinearAttentionDecoder(_Mixer):
@@ -226,7 +241,7 @@ class LinearAttentionDecoder(_Mixer):
 
     def step(self, q, k, v, gamma, slot, S_in, S_out, o, stream=None):
         n, w, (ldq, ldk, ldv, ldo) = self._B, self._w, self._ld
-        self._call(self._lib.bcmt_linattn_step, stream, self._rows("q", q, n, w, ldq),
+        self._call(self._lib.bcmt_linattn_step, self._stream(stream), self._rows("q", q, n, w, ldq),
                    self._rows("k", k, n, w, ldk), self._rows("v", v, n, w, ldv),
                    self._array("gamma", gamma, (self._H,), torch.float32),
                    self._array("slot", slot, (n,), torch.int32, True),
