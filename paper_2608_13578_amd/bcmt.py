@@ -477,29 +477,40 @@ def _scale(scale, dh):
     return float(scale) if scale is not None else float(dh) ** -0.5
 
 
+def _whole(bits, **values):
+    """The values as integers of a configuration; ctypes alone would cut off the bits
+    that do not fit."""
+    for name, x in values.items():
+        x = int(x)
+        if not -1 << (bits - 1) <= x < 1 << (bits - 1):
+            raise ValueError(f"{name}: {x} does not fit {bits} bits")
+        yield x
+
+
 def make_attn_config(total, nseq, H, Hkv, dh, dtype="bf16", scale=None, ldq=0, ldk=0, ldv=0,
                      ldo=0):
     """scale None: 1 / sqrt(dh); strides in elements, 0: dense rows."""
-    return bcmt_attn_config(int(total), int(nseq), int(H), int(Hkv), int(dh), _DTYPES[dtype],
-                            _scale(scale, dh), int(ldq), int(ldk), int(ldv), int(ldo))
+    return bcmt_attn_config(*_whole(32, total=total, nseq=nseq, H=H, Hkv=Hkv, dh=dh), _DTYPES[dtype],
+                            _scale(scale, dh), *_whole(64, ldq=ldq, ldk=ldk, ldv=ldv, ldo=ldo))
 
 
 def make_attn_decode_config(B, slots, cap, H, Hkv, dh, dtype="bf16", scale=None, ldq=0, ldk=0,
                             ldv=0, ldo=0, cs=0, ct=0, ch=0):
-    return bcmt_attn_decode_config(int(B), int(slots), int(cap), int(H), int(Hkv), int(dh),
-                                   _DTYPES[dtype], _scale(scale, dh), int(ldq), int(ldk), int(ldv),
-                                   int(ldo), int(cs), int(ct), int(ch))
+    return bcmt_attn_decode_config(
+        *_whole(32, B=B, slots=slots, cap=cap, H=H, Hkv=Hkv, dh=dh), _DTYPES[dtype],
+        _scale(scale, dh), *_whole(64, ldq=ldq, ldk=ldk, ldv=ldv, ldo=ldo, cs=cs, ct=ct, ch=ch))
 
 
 def make_linattn_config(total, nseq, H, dh, dtype="bf16", scale=None, ldq=0, ldk=0, ldv=0, ldo=0):
-    return bcmt_linattn_config(int(total), int(nseq), int(H), int(dh), _DTYPES[dtype],
-                               _scale(scale, dh), int(ldq), int(ldk), int(ldv), int(ldo))
+    return bcmt_linattn_config(*_whole(32, total=total, nseq=nseq, H=H, dh=dh), _DTYPES[dtype],
+                               _scale(scale, dh), *_whole(64, ldq=ldq, ldk=ldk, ldv=ldv, ldo=ldo))
 
 
 def make_linattn_step_config(B, slots, H, dh, dtype="bf16", scale=None, ldq=0, ldk=0, ldv=0,
                              ldo=0):
-    return bcmt_linattn_step_config(int(B), int(slots), int(H), int(dh), _DTYPES[dtype],
-                                    _scale(scale, dh), int(ldq), int(ldk), int(ldv), int(ldo))
+    return bcmt_linattn_step_config(*_whole(32, B=B, slots=slots, H=H, dh=dh), _DTYPES[dtype],
+                                    _scale(scale, dh),
+                                    *_whole(64, ldq=ldq, ldk=ldk, ldv=ldv, ldo=ldo))
 
 
 def bcmt_attn_validate(cfg):
