@@ -414,8 +414,9 @@ int bcmt_model_train_step(const bcmt_model_config* cfg, const int32_t* tokens,
  *   - Outputs must not overlap inputs or each other (columns of one array that
  *     do not meet are fine).
  *   - Everything is reduced in a fixed order: the same call gives the same bits.
- *   - dh is 16, 32, 64 or 128, total <= 2^30, nseq <= 65535 (else
- *     BCMT_ERR_UNSUPPORTED). */
+ *   - dh is 16, 32, 64 or 128; H and nseq <= 65535; (total / 64 + nseq) H < 2^23,
+ *     the division rounded down (else BCMT_ERR_UNSUPPORTED).  Row strides are at
+ *     most 2^28 elements (else BCMT_ERR_INVALID). */
 typedef struct {
   int32_t total;               /* rows of the packed arrays, >= 1 */
   int32_t nseq;                /* sequences, >= 1 */
@@ -451,7 +452,10 @@ int bcmt_attn_backward(const bcmt_attn_config* cfg, const void* q, const void* k
  * q, o: rows of H heads with strides ldq, ldo; k, v: rows of Hkv heads.  Both
  * caches: slot s, position t, head j at s cs + t ct + j ch elements; all 0 means
  * dense [slots, cap, Hkv, dh].  Otherwise each is positive and a multiple of 16
- * bytes, and no two entries may overlap.  slot, length: int32 on the device. */
+ * bytes, at least dh, and no two entries may overlap; in both forms slots cs +
+ * cap ct + Hkv ch <= 10^18 (else BCMT_ERR_INVALID).  slot, length: int32 on the
+ * device.  dh and the row strides as above; H <= 65535, cap and slots <= 2^30, and
+ * B Hkv ceil(H / Hkv / 16) <= 65535 (else BCMT_ERR_UNSUPPORTED). */
 typedef struct {
   int32_t B;      /* sequences of the batch, >= 1 */
   int32_t slots;  /* slots of the pool, >= 1 */
@@ -471,8 +475,8 @@ int bcmt_attn_decode(const bcmt_attn_decode_config* cfg, const void* q, const vo
 /* ------------------------------------------------ linear attention with decays
  * A decayed sum of key-value products, one decay gamma[h] in [0, 1] per head:
  *   S_t = gamma S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t
- * over packed sequences (cu, strides, overlap and errors as for the attention
- * above).  States are float32 [dh, dh] per head (rows along k, columns along v):
+ * over packed sequences (cu, strides, overlap, limits and errors as for the
+ * attention above).  States are float32 [dh, dh] per head (rows along k, columns along v):
  * S_in [nseq, H, dh, dh] is the state before each sequence's first row (NULL: 0),
  * S_out the state after its last (NULL: not wanted; it may be S_in).  A prompt
  * cut into pieces runs piece by piece on the states; an empty sequence passes its
@@ -504,7 +508,9 @@ int bcmt_linattn_backward(const bcmt_linattn_config* cfg, const void* q, const v
 /* One token per sequence: the state of slot slot[b] (NULL: b) of a pool S_in
  * [slots, H, dh, dh] advances into the same slot of S_out (which may be S_in; other
  * slots of S_out are not written).  A slot outside the pool gives a zero output row
- * and touches no state; two sequences must not share a slot. */
+ * and touches no state; two sequences must not share a slot.  dh and the row
+ * strides as above; H <= 65535, slots <= 2^30, B H < 2^23 (else
+ * BCMT_ERR_UNSUPPORTED). */
 typedef struct {
   int32_t B, slots, H, dh, dtype;
   float scale;
