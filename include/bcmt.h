@@ -482,6 +482,10 @@ int bcmt_attn_decode(const bcmt_attn_decode_config* cfg, const void* q, const vo
  * cut into pieces runs piece by piece on the states; an empty sequence passes its
  * state on.  gamma: H float32 on the device (0^0 is taken as 1), 4-byte aligned;
  * values outside [0, 1] give undefined numbers.
+ * States and their sums are float32.  In bf16 the decayed scores and the state before
+ * a block of rows are rounded to bf16 as operands of the products: each costs at most
+ * 2^-8 of the sum of magnitudes that makes up an element of o, dq, dk or dv, beside
+ * that element's own rounding.  S_out, dS_in and dgamma take no such rounding.
  * A value that is not finite reaches only its own row and later ones in the forward
  * pass; in the backward pass it may reach every gradient of its sequence. */
 typedef struct {

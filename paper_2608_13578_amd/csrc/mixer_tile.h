@@ -250,8 +250,10 @@ __device__ __forceinline__ SeqTile find_tile(const int* __restrict__ cu, int nse
 // sequence), so that no long tile starts when the chip is nearly done.  f(t) = sum
 // over sequences of max(0, tiles - t) items have index >= t; the largest t with
 // f(t) > x is the item's, and among the sequences that have it, x - f(t + 1) counts.
-// Up to 64 sequences, one a lane; more are walked slot by slot.  Items from f(0) on
-// are empty (tile < 0).
+// Up to 64 sequences, one a lane; more are walked slot by slot, which costs most
+// where one is long: sequences of 4096 and 63 times 128, 16 heads of 128 on 2, forward
+// 121 us and with an empty 65th 170 (12 heads of 64 on 4: 94 and 114); 64 of 16 to
+// 1024, gradients 844 and 1122 (312 and 376).  Items from f(0) on are empty (tile < 0).
 template <bool LAST>
 __device__ __forceinline__ SeqTile find_item(const int* __restrict__ cu, int nseq, int total,
                                              int TILE, int x) {

@@ -14,7 +14,7 @@
 // Register layouts (common.h): a matrix instruction returns lane l the column
 // l % 16 and rows 4 (l / 16) + r.  The forward and dQ compute transposed
 // scores, so a lane holds one query and a set of keys, and those registers are
-// the second operand of the next product as they are (Tile::col8 reads the
+// the second operand of the next product as they are (Tile::col_at reads the
 // first operand in the same key order).  dK/dV computes them untransposed,
 // one key per lane, to the same end.
 #include <algorithm>
@@ -86,11 +86,17 @@ struct PairLoads {
 // make a launch, NG = 2 teams of NW waves take the tiles in turn, each through its own
 // ring, and are joined in LDS at the end.
 //
-// The maximum is raised only when a score passes it by more than 2^kRaise: the
-// weights then stay below 2^kRaise (their relative rounding is the same at any
-// scale, and float32 sums have the room), and the outputs are rescaled, and the
-// lanes of a row agree on its maximum, in a few tiles of a sequence instead of
-// in all.  Tiles that every query of a wave sees whole take no mask.
+// The maximum is raised only when a score passes it by more than kRaise (both in
+// base-2 logarithms): the weights then stay below 2^kRaise (their relative rounding
+// is the same at any scale, and float32 sums have the room), and the outputs are
+// rescaled, and the lanes of a row agree on its maximum, in a few tiles of a
+// sequence instead of in all.  Tiles that every query of a wave sees whole take no
+// mask.
+//
+// In bfloat16 the weights are rounded to the type as operands of the product with
+// V, since the matrix instructions take no other; their sum l is of the float32
+// weights.  With the output's own rounding: an error of 1.8e-3 to 2.0e-3 in the
+// 2-norm, 1.6e-3 by the output's rounding alone.
 
 constexpr float kRaise = 8.f;
 
@@ -547,7 +553,8 @@ __global__ __launch_bounds__(NW * NG * 64, (DqShape<T, DH, NW, NG>::WAVES)) void
 // two waves and the keys with the most queries behind them are done sooner.
 // Shared heads are summed in registers, in a fixed order; where there are too
 // few workgroups for the chip, several take the steps of the same keys in turn
-// and leave float32 sums that a second kernel adds.
+// and leave float32 sums that a second kernel adds.  In bfloat16 the weights and dz
+// are rounded to the type as operands, as in the other two passes.
 
 template <typename T, int DH> struct KeyShape {
   static constexpr int NK = sizeof(T) == 2 ? 2 : 1;  // groups of 16 keys of a wave
@@ -786,7 +793,10 @@ __global__ __launch_bounds__(256) void seq_dkdv_sum_kernel(const int* __restrict
 }
 
 // Waves per head of a workgroup of NW: as many heads of a group share it as
-// divide the group, since their queries see the same keys.
+// divide the group, since their queries see the same keys; a power of two of them,
+// so that a group of 3 heads shares nothing.  Four sequences of 2048, 12 heads of 64
+// on 12, 4 and 3 (groups of 1, 3 and 4): forward 52, 51 and 51 us, gradients 149,
+// 150 and 158: the keys' traffic does not bound these.
 int waves_per_head(int NW, int G) {
   int hp = NW;
   while (G % hp) hp /= 2;
@@ -864,7 +874,9 @@ hipError_t dq_t(const SeqAttn& a, hipStream_t s) {
 // As many as the group has heads; more, up to 16, while a part has 8 rounds of its
 // teams (float32: 4, which take longer): a part costs the traffic of its float32 sums
 // (one sequence of 4096, 8 heads of 64 in bfloat16: 131 us with two parts, 146 with
-// one; two of 1024: 55 with four and 48 with one).
+// one; two of 1024: 55 with four and 48 with one).  The rounds are those of a sequence
+// of the mean length, since the host does not see the lengths: a long sequence among
+// short ones gets as few parts as they do.
 template <typename T, int DH>
 int parts_t(int total, int nseq, int Hkv, int G) {
   typedef KeyShape<T, DH> KS;
@@ -902,7 +914,8 @@ hipError_t bwd_t(const SeqAttn& a, hipStream_t s) {
 // maxima, sums and outputs are joined at the end.  The token's own key and
 // value are put into the tile that holds its position, whose later rows are
 // cleared (the cache may hold anything there); the wave that owns the tile
-// also writes them to the cache.
+// also writes them to the cache.  Weights are rounded to bfloat16 as in the prompt's
+// pass, with the same error (2.0e-3 to 2.1e-3 in the 2-norm).
 
 template <typename T, int DH> struct DecShape {
   // LDS of two buffers of K and V tiles per wave
@@ -1181,9 +1194,15 @@ hipError_t seq_attn_decode(DType dt, int dh, const DecAttn& a, hipStream_t s) {
 // 119 with two or eight per CU; 32 of 4096 each: 106, 105 and 119), at least two
 // tiles of every wave in a part, and no more parts than CUs, since the join reads
 // them all (one sequence of 131072, one head: 23 us with 256, 32 with 512).  Caches of
-// at most eight tiles a wave stay whole and need no second launch (12 heads of 64, one
-// and four parts: 512 positions 7.1 and 8.6 us, 1024 positions 9.7 and 8.6, but 11.6
-// and 14.4 called from a host; 32 sequences of up to 1024, 8 heads of 128: 18 and 29).
+// at most eight tiles a wave stay whole and need no second launch: a conversation fills
+// its cache, and over its course one part costs a captured graph as much as several,
+// and a host that makes the calls one by one less.  In us, one sequence whose cache is
+// a quarter, half, three quarters and all full, in one part | in four or more:
+//   12 heads of 64,      1024: 5.5  6.9  8.2  9.5 |  7.5  7.6  8.3  8.3, from a host 8.5 to 9.5 | 11.5
+//                        2048: 6.9  9.5 12.1 14.9 |  7.7  7.8  8.5  8.6,            8.4 to 14.9 | 11.5
+//   32 heads of 128 on 8, 1024: 7.1  9.2 11.2 13.2 |  8.8  9.0  9.9 10.2,            8.3 to 13.1 | 11.4
+//                        2048: 9.2 13.1 17.3 21.2 |  8.9  9.0 10.1 10.2,            9.3 to 21.1 | 11.4
+// 32 sequences of up to 1024, 8 heads of 128: 18 us in one part and 29 in four.
 int seq_attn_decode_splits(DType dt, int dh, int B, int H, int Hkv, int cap) {
   const int G = H / Hkv, NH = (G + 15) / 16;
   const int nw = (dt == DType::BF16 ? 2 : 4) * dh >= 512 ? 2 : 4;
